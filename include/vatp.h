@@ -115,6 +115,26 @@ typedef struct {
                                  re-read that one row                                            */
 } vatp_cache;
 
+/*
+ * The decode state with K and V rows in 4 bits (host struct of caller-owned DEVICE arrays).
+ * state: as vatp_cache, except that k_cache and v_cache hold codes, [batch, kv heads, cap, head_dim / 2] bytes.
+ * k_params, v_params: [batch, kv heads, cap, head_dim / 32] pairs (scale, low end) of bf16, 16-byte aligned.
+ *
+ * A row consists of groups of 32 consecutive channels.  A group with values x (in fp32) is stored as
+ *   lo   = the largest bf16 that is not above min x
+ *   sc   = the smallest bf16 that is not below (max x - lo) / 15;  0 where that is below 2^-100
+ *   code = rint((x - lo) * (1 / sc)), ties to even, at most 15;    0 where sc = 0
+ * with the difference, the quotients and the product each rounded to fp32, and stands for lo + code * sc.  No value is clamped,
+ * and |x - (lo + code * sc)| <= sc / 2 up to fp32 rounding.  Values are assumed below 2^126 in magnitude.
+ * Channel 32 g + 4 j + e (j < 8, e < 4) is a nibble of byte j * (head_dim / 16) + 2 g + e / 2 of the row, the low nibble for an
+ * even e: sixteen bytes in a row hold the same channels of all groups, which is how the generation step reads them.
+ * With head_dim 128 a row takes 64 + 16 bytes (256 in bf16).
+ */
+typedef struct {
+  vatp_cache state;
+  void *k_params, *v_params;
+} vatp_cache_q4;
+
 /* Slots per unit of the decode state for a budget of B tokens (see vatp_cache). */
 int32_t vatp_cache_capacity(int32_t budget);
 
@@ -296,6 +316,59 @@ vatp_status vatp_compact_window(const vatp_params* params, const void* q, const 
 vatp_status vatp_decode_step(const vatp_params* params, const vatp_cache* cache, const void* q_new,
                              const void* k_new, const void* v_new, void* out, int32_t* evicted_pos,
                              int32_t* dev_status, void* cuda_stream);
+
+/*
+ * vatp_compact into the 4-bit state: the kept rows are quantised on their way, everything else is initialised as there.  Rows of
+ * slots that receive no token are left alone.  (The paper has no counterpart; nor have the five calls below.)
+ * With VATP_IND_WINDOW win_rows is required, as for vatp_compact; grouped queries with a history window go through
+ * vatp_compact_window and vatp_cache_pack_q4 (VATP_ERR_UNSUPPORTED here).
+ */
+vatp_status vatp_compact_q4(const vatp_params* params, const void* k, const void* v, const float* attn_acc,
+                            const float* vnorm, const float* win_rows, const int32_t* kept_idx,
+                            const vatp_cache_q4* cache, int32_t* dev_status, void* cuda_stream);
+
+/*
+ * A decode state with rows of the params dtype into one with 4-bit rows, and back (the rows' values, rounded to the params dtype
+ * once).  Both states have params->batch entries and params->budget.  Rows of slots that hold a token are converted, others left
+ * alone; all else of the state is copied, except for arrays that both structs share (a program that keeps both forms of the rows
+ * over one set of acc, vnorm, pos, ... arrays): those stay as they are.  ring and acc_fixed must be 16-byte aligned.  Rows in the
+ * two forms may not overlap, nor may arrays overlap their counterparts without being the same (VATP_ERR_INVALID_ARG).
+ * seq_len in params is ignored.
+ */
+vatp_status vatp_cache_pack_q4(const vatp_params* params, const vatp_cache* from, const vatp_cache_q4* to,
+                               int32_t* dev_status, void* cuda_stream);
+vatp_status vatp_cache_unpack_q4(const vatp_params* params, const vatp_cache_q4* from, const vatp_cache* to,
+                                 int32_t* dev_status, void* cuda_stream);
+
+/*
+ * vatp_decode_step on the 4-bit state.  The incoming row is quantised when it is stored and takes part as stored, like every other
+ * row; its norm (Eq. 4) is that of k_new's and v_new's values as given.  Up to eight query heads per KV head
+ * (VATP_ERR_UNSUPPORTED beyond, and for budgets whose logits do not fit into the shared memory of the CTAs of a unit).
+ * Everything else is as in vatp_decode_step, except that VATP_FLAG_DECODE_OVERLAP has no effect: every step waits for all earlier
+ * work in the stream.
+ */
+vatp_status vatp_decode_step_q4(const vatp_params* params, const vatp_cache_q4* cache, const void* q_new,
+                                const void* k_new, const void* v_new, void* out, int32_t* evicted_pos,
+                                int32_t* dev_status, void* cuda_stream);
+
+/*
+ * Entries (sequences: all KV heads, rows and state) of `from` into entries of `to`: fork a prompt into samples, reorder or compact
+ * a batch, let a sequence join a batch, free entries.
+ * src_of: [params->batch] int32 device array; entry b of `to` becomes a copy of entry src_of[b] of `from`, bit for bit;
+ *   VATP_SEQ_KEEP leaves it as it is; VATP_SEQ_FREE empties it (no tokens, next_pos 0; its rows are left alone).
+ * params describes `to`; `from` has from_batch entries and from_budget, which may be another one: the slots that both have are
+ * copied, further slots of `to` hold no token.  An entry with more than params->budget tokens does not fit.
+ * `from` and `to` either are the same state (all arrays the same; an entry may then only be read where no entry overwrites it:
+ * src_of[src_of[b]] is itself or VATP_SEQ_KEEP) or share no memory.  What the host cannot see - a source outside `from`, an entry
+ * that does not fit or that is overwritten - leaves the entry as it is and writes VATP_ERR_INVALID_ARG to *dev_status.
+ * ring and acc_fixed must be 16-byte aligned.  seq_len in params is ignored.
+ */
+enum { VATP_SEQ_FREE = -1, VATP_SEQ_KEEP = -2 };
+vatp_status vatp_cache_copy(const vatp_params* params, const vatp_cache* from, int32_t from_batch, int32_t from_budget,
+                            const vatp_cache* to, const int32_t* src_of, int32_t* dev_status, void* cuda_stream);
+vatp_status vatp_cache_copy_q4(const vatp_params* params, const vatp_cache_q4* from, int32_t from_batch,
+                               int32_t from_budget, const vatp_cache_q4* to, const int32_t* src_of, int32_t* dev_status,
+                               void* cuda_stream);
 
 /*
  * Self-test of the bounded device-side waits (every pipeline wait in this library gives up after a

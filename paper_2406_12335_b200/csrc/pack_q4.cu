@@ -1,0 +1,205 @@
+// Rows of K and V to and from their 4-bit form: compaction of a prompt's kept rows, conversion of a decode state, and back.
+//
+// Both are bound by memory: a row of 128 bf16 channels is 256 bytes in one form and 80 in the other.
+#include "q4.cuh"
+
+namespace vatp {
+namespace {
+
+constexpr int PK_WARPS = 8, PK_THREADS = PK_WARPS * 32;
+
+// sixteen consecutive channels
+__device__ __forceinline__ void load16(const __nv_bfloat16* p, float (&x)[16]) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const uint4 r = load_behind_wait(reinterpret_cast<const uint4*>(p) + i);
+    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      x[8 * i + 2 * k] = __uint_as_float(w[k] << 16);
+      x[8 * i + 2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u);
+    }
+  }
+}
+__device__ __forceinline__ void load16(const float* p, float (&x)[16]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float4 r = load_behind_wait(reinterpret_cast<const float4*>(p) + i);
+    x[4 * i] = r.x; x[4 * i + 1] = r.y; x[4 * i + 2] = r.z; x[4 * i + 3] = r.w;
+  }
+}
+
+// A warp takes 512 / HD consecutive slots of a unit, HD / 16 lanes a row: a lane has half a group, finds its least and largest value
+// with one exchange, and its codes pass through 256 bytes of shared memory so that they leave as full 16-byte words.
+// kept != nullptr (compaction): slot s of unit u takes row kept[u][s] of the prompt, and the decode state is initialised.
+// kept == nullptr (conversion): slot s takes slot s of the cache k, v where pos_from says that it holds a token.
+template <typename T, int HD>
+__global__ void __launch_bounds__(PK_THREADS)
+pack_q4_kernel(Shape sh, int B, int cap, int blocks_per_unit, const T* k, const T* v, const int32_t* kept, const int32_t* pos_from,
+               const float* attn_acc, const float* vnorm, vatp_cache_q4 c, int32_t* dev_status) {
+  constexpr int LPR = HD / 16, ROWS = 32 / LPR;                  // lanes a row, rows of a warp
+  __shared__ __align__(16) unsigned char stage[PK_WARPS][2][256];
+  const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+  const int u = blockIdx.x / blocks_per_unit;
+  const int first = ((blockIdx.x - u * blocks_per_unit) * PK_WARPS + wid) * ROWS;      // this warp's first slot
+  const int sub = lane % LPR, g = sub >> 1, h = sub & 1;          // this lane's group and half of it
+  const int s = first + lane / LPR;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  if (first >= cap) return;
+  const int len = min(sh.T, B);
+  const int64_t o = (int64_t)u * cap + s;
+  int64_t from = -1;                                              // element offset of the row in k and v
+  if (kept) {
+    int src = s < len ? kept[(int64_t)u * B + s] : -1;
+    if (src >= 0 && !VATP_INB(src, sh.T, dev_status)) src = -1;
+    if (src >= 0) from = unit_offset(sh, u) + (int64_t)src * sh.st;
+    if (sub == 0 && s < cap) {
+      c.state.pos[o] = src;
+      c.state.acc[o] = src >= 0 ? attn_acc[(int64_t)u * sh.T + src] : 0.f;
+      c.state.vnorm[o] = src >= 0 ? vnorm[(int64_t)u * sh.T + src] : 0.f;
+      if (s == 0) {
+        c.state.len[u] = len;
+        c.state.free_slot[u] = len;
+        c.state.next_pos[u] = sh.T;
+        c.state.last_slot[u] = -1;
+      }
+    }
+  } else if (s < cap && pos_from[o] >= 0) {
+    from = o * HD;
+  }
+  float x[2][16];
+  if (from >= 0) {
+    load16(k + from + 32 * g + 16 * h, x[0]);
+    load16(v + from + 32 * g + 16 * h, x[1]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[0][i] = x[1][i] = 0.f;
+  }
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    float mn = x[t][0], mx = x[t][0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) { mn = fminf(mn, x[t][i]); mx = fmaxf(mx, x[t][i]); }
+    mn = fminf(mn, __shfl_xor_sync(0xffffffffu, mn, 1));
+    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+    const Q4Group q = q4_group(mn, mx);
+    if (from >= 0 && h == 0) reinterpret_cast<uint32_t*>(t ? c.v_params : c.k_params)[o * (HD / 32) + g] = q4_params(q);
+    unsigned char* row = stage[wid][t] + (lane / LPR) * (HD / 2);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      uint32_t code = 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) code |= q4_code(q, x[t][4 * j + e]) << (4 * e);
+      *reinterpret_cast<uint16_t*>(row + q4_byte<HD>(g, 4 * h + j)) = (uint16_t)code;
+    }
+  }
+  const uint32_t rows = __ballot_sync(0xffffffffu, from >= 0 && sub == 0);      // bit LPR * r: row r is live
+  __syncwarp();
+  const int t = lane >> 4, at = (lane & 15) * 16, r = at / (HD / 2);            // lanes 0-15 K, 16-31 V
+  if (rows >> (LPR * r) & 1u) {
+    unsigned char* dst = static_cast<unsigned char*>(t ? c.state.v_cache : c.state.k_cache) + ((int64_t)u * cap + first) * (HD / 2) + at;
+    *reinterpret_cast<uint4*>(dst) = *reinterpret_cast<const uint4*>(stage[wid][t] + at);
+  }
+}
+
+__device__ __forceinline__ void store4(__nv_bfloat16* p, const float (&x)[4]) {
+  __nv_bfloat162 a = __floats2bfloat162_rn(x[0], x[1]), b = __floats2bfloat162_rn(x[2], x[3]);
+  *reinterpret_cast<uint2*>(p) = make_uint2(reinterpret_cast<uint32_t&>(a), reinterpret_cast<uint32_t&>(b));
+}
+__device__ __forceinline__ void store4(float* p, const float (&x)[4]) { *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]); }
+
+// A lane takes HD / 16 bytes of a row, i.e. four channels of each of its groups; eight lanes a row.  A warp's stores of one group
+// cover four rows, 64 or 128 bytes each.
+template <typename T, int HD>
+__global__ void __launch_bounds__(PK_THREADS)
+unpack_q4_kernel(int64_t slots, vatp_cache_q4 c, T* k, T* v) {
+  constexpr int G = HD / 32;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int64_t i = (int64_t)blockIdx.x * (PK_THREADS / 8) + threadIdx.x / 8;    // the slot
+  const int j = threadIdx.x & 7;
+  if (i >= slots || c.state.pos[i] < 0) return;
+  uint32_t w[2][G / 2], pr[2][G];
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    const unsigned char* codes = static_cast<const unsigned char*>(t ? c.state.v_cache : c.state.k_cache) + i * (HD / 2) + j * (HD / 16);
+    const uint32_t* params = static_cast<const uint32_t*>(t ? c.v_params : c.k_params) + i * G;
+#pragma unroll
+    for (int x = 0; x < G / 2; ++x) w[t][x] = load_behind_wait(reinterpret_cast<const uint32_t*>(codes) + x);
+#pragma unroll
+    for (int x = 0; x < G; ++x) pr[t][x] = load_behind_wait(params + x);
+  }
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      const uint32_t code = w[t][g / 2] >> (16 * (g & 1));
+      float x[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = fmaf((float)(code >> (4 * e) & 15u), q4_scale(pr[t][g]), q4_low(pr[t][g]));
+      store4((t ? v : k) + i * HD + 32 * g + 4 * j, x);
+    }
+}
+
+// Windowed indicator state of the kept tokens, as compact.cu's ring_kernel leaves it: ring[u][(T - w + r) mod w][slot] =
+// win_rows[u][r][kept[slot]] and the exact fixed-point sum of every slot.
+__global__ void ring_q4_kernel(int T, int w, int B, int cap, const float* __restrict__ win_rows, const int32_t* __restrict__ kept,
+                               vatp_cache c, int32_t* dev_status) {
+  const int per_unit = (cap + blockDim.x - 1) / blockDim.x, u = blockIdx.x / per_unit;
+  const int slot = (blockIdx.x - u * per_unit) * blockDim.x + threadIdx.x;
+  if (slot >= cap) return;
+  int src = slot < min(T, B) ? kept[(int64_t)u * B + slot] : -1;
+  if (src >= 0 && !VATP_INB(src, T, dev_status)) src = -1;
+  long long fx = 0;
+  for (int r = 0; r < w; ++r) {
+    const int j = T - w + r;                 // query position of this window row (may be < 0)
+    const float p = src >= 0 && j >= 0 ? win_rows[((int64_t)u * w + r) * T + src] : 0.f;
+    c.ring[((int64_t)u * w + ((j % w) + w) % w) * cap + slot] = p;
+    fx += prob_to_fixed(p);
+  }
+  c.acc_fixed[(int64_t)u * cap + slot] = fx;
+  c.acc[(int64_t)u * cap + slot] = fixed_to_prob(fx);
+}
+
+template <typename T, int HD>
+cudaError_t pack_hd(const Shape& s, int B, const void* k, const void* v, const int32_t* kept, const int32_t* pos_from, const float* attn_acc,
+                    const float* vnorm, const vatp_cache_q4& c, int32_t* dev_status, cudaStream_t st) {
+  constexpr int SLOTS = PK_WARPS * 512 / HD;       // of a CTA
+  const int cap = cache_capacity(B), per_unit = (cap + SLOTS - 1) / SLOTS;
+  if ((int64_t)s.units * per_unit > 0x7fffffffll) return cudaErrorInvalidValue;
+  DependentLaunch dl(dim3((unsigned)(s.units * per_unit)), dim3(PK_THREADS), 0, st);
+  return cudaLaunchKernelEx(&dl.cfg, pack_q4_kernel<T, HD>, s, B, cap, per_unit, (const T*)k, (const T*)v, kept, pos_from, attn_acc, vnorm, c, dev_status);
+}
+
+template <typename T, int HD>
+cudaError_t unpack_hd(int units, int B, const vatp_cache_q4& c, void* k, void* v, cudaStream_t st) {
+  const int64_t slots = (int64_t)units * cache_capacity(B), ctas = (slots + PK_THREADS / 8 - 1) / (PK_THREADS / 8);
+  if (ctas > 0x7fffffffll) return cudaErrorInvalidValue;
+  DependentLaunch dl(dim3((unsigned)ctas), dim3(PK_THREADS), 0, st);
+  return cudaLaunchKernelEx(&dl.cfg, unpack_q4_kernel<T, HD>, slots, c, (T*)k, (T*)v);
+}
+
+}  // namespace
+
+cudaError_t launch_pack_q4(const Shape& s, int dtype, int B, const void* k, const void* v, const int32_t* kept, const int32_t* pos_from,
+                           const float* attn_acc, const float* vnorm, const float* win_rows, const vatp_cache_q4& c,
+                           int32_t* dev_status, cudaStream_t st) {
+  auto f = dtype == VATP_F32 ? (s.d == 64 ? pack_hd<float, 64> : pack_hd<float, 128>)
+                             : (s.d == 64 ? pack_hd<__nv_bfloat16, 64> : pack_hd<__nv_bfloat16, 128>);
+  cudaError_t e = f(s, B, k, v, kept, pos_from, attn_acc, vnorm, c, dev_status, st);
+  if (e == cudaSuccess && kept && s.window > 0) {
+    const int cap = cache_capacity(B);
+    const int64_t ctas = (int64_t)s.units * ((cap + 127) / 128);
+    if (ctas > 0x7fffffffll) return cudaErrorInvalidValue;
+    ring_q4_kernel<<<(unsigned)ctas, 128, 0, st>>>(s.T, s.window, B, cap, win_rows, kept, c.state, dev_status);
+    e = cudaGetLastError();
+  }
+  return e;
+}
+
+cudaError_t launch_unpack_q4(int units, int d, int dtype, int B, const vatp_cache_q4& c, void* k, void* v, cudaStream_t st) {
+  auto f = dtype == VATP_F32 ? (d == 64 ? unpack_hd<float, 64> : unpack_hd<float, 128>)
+                             : (d == 64 ? unpack_hd<__nv_bfloat16, 64> : unpack_hd<__nv_bfloat16, 128>);
+  return f(units, B, c, k, v, st);
+}
+
+}  // namespace vatp

@@ -84,6 +84,113 @@ bool cache_ok(const vatp_cache* c, bool windowed) {
   return true;
 }
 
+bool cache_q4_ok(const vatp_cache_q4* c, bool windowed) {
+  return c && cache_ok(&c->state, windowed) && c->k_params && c->v_params && aligned16(c->k_params) && aligned16(c->v_params);
+}
+
+// The arrays of two decode states side by side, rows first: bytes per slot and unit are the states' own.  `rows`: the arrays that
+// hold K and V rows are wanted too (both states have them in the same form).
+struct StatePair {
+  CacheArray a[MAX_CACHE_ARRAYS];
+  int n = 0, shared = 0, apart = 0;
+  bool ok = true;
+  int64_t from_units, to_units;
+  int from_cap, to_cap;
+  // an array is either the same in both states or lies apart from its counterpart
+  void bytes(const void* from, const void* to, int64_t from_bytes, int64_t to_bytes) {
+    const uintptr_t f = reinterpret_cast<uintptr_t>(from), t = reinterpret_cast<uintptr_t>(to);
+    if (f == t) ++shared;
+    else if (f < t + (uintptr_t)to_bytes && t < f + (uintptr_t)from_bytes) ok = false;
+    else ++apart;
+  }
+  void slots(const void* from, void* to, int rows, int slot_bytes) {
+    if (!aligned16(from) || !aligned16(to)) ok = false;
+    bytes(from, to, from_units * rows * from_cap * slot_bytes, to_units * rows * to_cap * slot_bytes);
+    a[n++] = CacheArray{from, to, rows, slot_bytes};
+  }
+  StatePair(const vatp_cache& f, const vatp_cache& t, int64_t fu, int64_t tu, int fc, int tc, int window) : from_units(fu), to_units(tu), from_cap(fc), to_cap(tc) {
+    slots(f.acc, t.acc, 1, 4);
+    slots(f.vnorm, t.vnorm, 1, 4);
+    slots(f.pos, t.pos, 1, 4);
+    if (window > 0) {
+      slots(f.ring, t.ring, window, 4);
+      slots(f.acc_fixed, t.acc_fixed, 1, 8);
+    }
+    bytes(f.len, t.len, fu * 4, tu * 4);
+    bytes(f.free_slot, t.free_slot, fu * 4, tu * 4);
+    bytes(f.next_pos, t.next_pos, fu * 4, tu * 4);
+    bytes(f.last_slot, t.last_slot, fu * 4, tu * 4);
+  }
+};
+
+// Rows in one form and the same rows in the other may not overlap.
+bool rows_apart(const void* a, int64_t a_bytes, const void* b, int64_t b_bytes) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x >= y + (uintptr_t)b_bytes || y >= x + (uintptr_t)a_bytes;
+}
+
+// vatp_cache_pack_q4 (pack) and vatp_cache_unpack_q4: rows by one launch, then the state's arrays that are not shared
+vatp_status convert_q4(const vatp_params* p, const vatp_cache* wide, const vatp_cache_q4* narrow, bool pack, int32_t* dev_status, void* cuda_stream) {
+  vatp_status s = check_params(p, false);
+  if (s != VATP_OK) return s;
+  const bool windowed = p->indicator == VATP_IND_WINDOW;
+  if (!cache_ok(wide, windowed) || !cache_q4_ok(narrow, windowed)) return VATP_ERR_INVALID_ARG;
+  const int cap = cache_capacity(p->budget), d = p->head_dim;
+  const int64_t units = (int64_t)p->batch * kv_heads_of(p), wide_bytes = units * cap * d * (p->dtype == VATP_F32 ? 4 : 2);
+  const void* w[2] = {wide->k_cache, wide->v_cache};
+  const void* codes[2] = {narrow->state.k_cache, narrow->state.v_cache};
+  const void* params[2] = {narrow->k_params, narrow->v_params};
+  for (int i = 0; i < 2; ++i)
+    for (int j = 0; j < 2; ++j)
+      if (!rows_apart(w[i], wide_bytes, codes[j], units * cap * (d / 2)) || !rows_apart(w[i], wide_bytes, params[j], units * cap * (d / 8)))
+        return VATP_ERR_INVALID_ARG;
+  const vatp_cache &from = pack ? *wide : narrow->state, &to = pack ? narrow->state : *wide;
+  const StatePair pair(from, to, units, units, cap, cap, windowed ? p->window_w : 0);
+  if (!pair.ok) return VATP_ERR_INVALID_ARG;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  decode_history_forget(st);
+  cudaError_t e;
+  if (pack) {
+    Shape sh;
+    std::memset(&sh, 0, sizeof(sh));
+    sh.units = (int)units;
+    sh.d = d;
+    e = launch_pack_q4(sh, p->dtype, p->budget, w[0], w[1], nullptr, from.pos, nullptr, nullptr, nullptr, *narrow, dev_status, st);
+  } else {
+    e = launch_unpack_q4((int)units, d, p->dtype, p->budget, *narrow, wide->k_cache, wide->v_cache, st);
+  }
+  if (e == cudaSuccess && pair.apart)
+    e = launch_cache_copy((int)units, kv_heads_of(p), p->batch, p->budget, p->budget, pair.a, pair.n, nullptr, false, from, to, dev_status, st);
+  return e == cudaSuccess ? VATP_OK : VATP_ERR_CUDA;
+}
+
+// vatp_cache_copy and vatp_cache_copy_q4; params arrays: null for 16- and 32-bit rows
+vatp_status copy_impl(const vatp_params* p, const vatp_cache* from, const void* from_params[2], int32_t from_batch, int32_t from_budget,
+                      const vatp_cache* to, void* const to_params[2], const int32_t* src_of, int32_t* dev_status, void* cuda_stream) {
+  vatp_status s = check_params(p, false);
+  if (s != VATP_OK) return s;
+  const bool windowed = p->indicator == VATP_IND_WINDOW;
+  if (!cache_ok(from, windowed) || !cache_ok(to, windowed) || !src_of || from_batch <= 0 || from_budget <= 0) return VATP_ERR_INVALID_ARG;
+  const int kvh = kv_heads_of(p), d = p->head_dim;
+  const int64_t fu = (int64_t)from_batch * kvh, tu = (int64_t)p->batch * kvh;
+  StatePair pair(*from, *to, fu, tu, cache_capacity(from_budget), cache_capacity(p->budget), windowed ? p->window_w : 0);
+  const int row = from_params ? d / 2 : d * (p->dtype == VATP_F32 ? 4 : 2);
+  pair.slots(from->k_cache, to->k_cache, 1, row);
+  pair.slots(from->v_cache, to->v_cache, 1, row);
+  if (from_params) {
+    pair.slots(from_params[0], to_params[0], 1, d / 8);
+    pair.slots(from_params[1], to_params[1], 1, d / 8);
+  }
+  // within one state (all arrays the same) or between two (none)
+  if (!pair.ok || (pair.shared && pair.apart)) return VATP_ERR_INVALID_ARG;
+  const bool in_place = pair.shared > 0;
+  if (in_place && (from_batch != p->batch || from_budget != p->budget)) return VATP_ERR_INVALID_ARG;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  decode_history_forget(st);
+  const cudaError_t e = launch_cache_copy((int)tu, kvh, from_batch, from_budget, p->budget, pair.a, pair.n, src_of, in_place, *from, *to, dev_status, st);
+  return e == cudaSuccess ? VATP_OK : VATP_ERR_CUDA;
+}
+
 // The prefill entry points: lse_in == nullptr runs pass 1, otherwise the caller's normalisers replace it;
 // attn_out != nullptr runs the attention forward in pass 1's place (it yields the same normalisers).
 vatp_status prefill_impl(const vatp_params* p, const void* q, const void* k, const void* v, const float* lse_in,
@@ -309,6 +416,62 @@ vatp_status vatp_decode_step(const vatp_params* p, const vatp_cache* cache, cons
                                 evicted_pos, dev_status, static_cast<cudaStream_t>(cuda_stream),
                                 (p->flags & VATP_FLAG_DECODE_OVERLAP) != 0);
   return e == cudaSuccess ? VATP_OK : VATP_ERR_CUDA;
+}
+
+vatp_status vatp_compact_q4(const vatp_params* p, const void* k, const void* v, const float* attn_acc, const float* vnorm,
+                            const float* win_rows, const int32_t* kept_idx, const vatp_cache_q4* cache, int32_t* dev_status,
+                            void* cuda_stream) {
+  vatp_status s = check_params(p, true);
+  if (s != VATP_OK) return s;
+  const bool windowed = p->indicator == VATP_IND_WINDOW;
+  if (!k || !v || !attn_acc || !vnorm || !kept_idx || !cache_q4_ok(cache, windowed)) return VATP_ERR_INVALID_ARG;
+  if (windowed && !win_rows) return VATP_ERR_INVALID_ARG;
+  if (windowed && group_of(p) > 1) return VATP_ERR_UNSUPPORTED;
+  if (!aligned16(k) || !aligned16(v)) return VATP_ERR_INVALID_ARG;
+  Shape sh;
+  s = make_shape(p, &sh);
+  if (s != VATP_OK) return s;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  decode_history_forget(st);
+  const cudaError_t e = launch_pack_q4(sh, p->dtype, p->budget, k, v, kept_idx, nullptr, attn_acc, vnorm, win_rows, *cache, dev_status, st);
+  return e == cudaSuccess ? VATP_OK : VATP_ERR_CUDA;
+}
+
+vatp_status vatp_cache_pack_q4(const vatp_params* p, const vatp_cache* from, const vatp_cache_q4* to, int32_t* dev_status, void* cuda_stream) {
+  return convert_q4(p, from, to, true, dev_status, cuda_stream);
+}
+
+vatp_status vatp_cache_unpack_q4(const vatp_params* p, const vatp_cache_q4* from, const vatp_cache* to, int32_t* dev_status, void* cuda_stream) {
+  return convert_q4(p, to, from, false, dev_status, cuda_stream);
+}
+
+vatp_status vatp_decode_step_q4(const vatp_params* p, const vatp_cache_q4* cache, const void* q_new, const void* k_new, const void* v_new,
+                                void* out, int32_t* evicted_pos, int32_t* dev_status, void* cuda_stream) {
+  vatp_status s = check_params(p, false);
+  if (s != VATP_OK) return s;
+  const bool windowed = p->indicator == VATP_IND_WINDOW;
+  if (!q_new || !k_new || !v_new || !out || !cache_q4_ok(cache, windowed)) return VATP_ERR_INVALID_ARG;
+  if (!aligned16(q_new) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(out)) return VATP_ERR_INVALID_ARG;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  decode_history_forget(st);
+  const cudaError_t e = launch_decode_q4(p->batch * kv_heads_of(p), group_of(p), p->head_dim, p->dtype, p->budget, p->n_sink, p->n_recent,
+                                         windowed ? p->window_w : 0, p->norm_kind, p->scale, *cache, q_new, k_new, v_new, out, evicted_pos,
+                                         dev_status, st);
+  return e == cudaSuccess ? VATP_OK : (e == cudaErrorNotSupported ? VATP_ERR_UNSUPPORTED : VATP_ERR_CUDA);
+}
+
+vatp_status vatp_cache_copy(const vatp_params* p, const vatp_cache* from, int32_t from_batch, int32_t from_budget, const vatp_cache* to,
+                            const int32_t* src_of, int32_t* dev_status, void* cuda_stream) {
+  return copy_impl(p, from, nullptr, from_batch, from_budget, to, nullptr, src_of, dev_status, cuda_stream);
+}
+
+vatp_status vatp_cache_copy_q4(const vatp_params* p, const vatp_cache_q4* from, int32_t from_batch, int32_t from_budget, const vatp_cache_q4* to,
+                               const int32_t* src_of, int32_t* dev_status, void* cuda_stream) {
+  const bool windowed = p && p->indicator == VATP_IND_WINDOW;
+  if (!cache_q4_ok(from, windowed) || !cache_q4_ok(to, windowed)) return VATP_ERR_INVALID_ARG;
+  const void* from_params[2] = {from->k_params, from->v_params};
+  void* const to_params[2] = {to->k_params, to->v_params};
+  return copy_impl(p, &from->state, from_params, from_batch, from_budget, &to->state, to_params, src_of, dev_status, cuda_stream);
 }
 
 }  // extern "C"

@@ -23,6 +23,7 @@ NORM_KINDS = {"l1": 0, "l2": 1, "linf": 2}
 FLAG_DECODE_OVERLAP = 1
 STATIC_SCRATCH_BYTES = (4 << 20) + 256
 EXPORTS = ["vatp_cache_capacity", "vatp_workspace_bytes", "vatp_prefill_scores", "vatp_prefill_scores_from_lse", "vatp_prefill_attention_scores", "vatp_prefill_scores_static", "vatp_select", "vatp_compact", "vatp_compact_window", "vatp_decode_step",
+           "vatp_compact_q4", "vatp_cache_pack_q4", "vatp_cache_unpack_q4", "vatp_decode_step_q4", "vatp_cache_copy", "vatp_cache_copy_q4",
            "vatp_selftest_bounded_wait", "vatp_selftest_overlap_policy", "vatp_status_string"]
 
 
@@ -38,6 +39,12 @@ class CacheStruct(C.Structure):
                 ("pos", C.c_void_p), ("len", C.c_void_p), ("free_slot", C.c_void_p), ("next_pos", C.c_void_p),
                 ("ring", C.c_void_p), ("acc_fixed", C.c_void_p), ("last_slot", C.c_void_p)]
 
+
+class CacheQ4Struct(C.Structure):
+    _fields_ = [("state", CacheStruct), ("k_params", C.c_void_p), ("v_params", C.c_void_p)]
+
+
+SEQ_FREE, SEQ_KEEP = -1, -2        # entries of vatp_cache_copy's map that name no source
 
 _vp = C.c_void_p
 lib.vatp_cache_capacity.restype = C.c_int32
@@ -60,6 +67,18 @@ lib.vatp_compact_window.restype = C.c_int
 lib.vatp_compact_window.argtypes = [C.POINTER(Params), _vp, _vp, _vp, _vp, _vp, _vp, _vp, C.POINTER(CacheStruct), _vp, _vp]
 lib.vatp_decode_step.restype = C.c_int
 lib.vatp_decode_step.argtypes = [C.POINTER(Params), C.POINTER(CacheStruct), _vp, _vp, _vp, _vp, _vp, _vp, _vp]
+lib.vatp_compact_q4.restype = C.c_int
+lib.vatp_compact_q4.argtypes = [C.POINTER(Params), _vp, _vp, _vp, _vp, _vp, _vp, C.POINTER(CacheQ4Struct), _vp, _vp]
+lib.vatp_cache_pack_q4.restype = C.c_int
+lib.vatp_cache_pack_q4.argtypes = [C.POINTER(Params), C.POINTER(CacheStruct), C.POINTER(CacheQ4Struct), _vp, _vp]
+lib.vatp_cache_unpack_q4.restype = C.c_int
+lib.vatp_cache_unpack_q4.argtypes = [C.POINTER(Params), C.POINTER(CacheQ4Struct), C.POINTER(CacheStruct), _vp, _vp]
+lib.vatp_decode_step_q4.restype = C.c_int
+lib.vatp_decode_step_q4.argtypes = [C.POINTER(Params), C.POINTER(CacheQ4Struct), _vp, _vp, _vp, _vp, _vp, _vp, _vp]
+lib.vatp_cache_copy.restype = C.c_int
+lib.vatp_cache_copy.argtypes = [C.POINTER(Params), C.POINTER(CacheStruct), C.c_int32, C.c_int32, C.POINTER(CacheStruct), _vp, _vp, _vp]
+lib.vatp_cache_copy_q4.restype = C.c_int
+lib.vatp_cache_copy_q4.argtypes = [C.POINTER(Params), C.POINTER(CacheQ4Struct), C.c_int32, C.c_int32, C.POINTER(CacheQ4Struct), _vp, _vp, _vp]
 lib.vatp_selftest_bounded_wait.restype = C.c_int
 lib.vatp_selftest_bounded_wait.argtypes = [C.c_uint64, _vp, _vp, _vp]
 lib.vatp_selftest_overlap_policy.restype = C.c_int32
@@ -117,15 +136,19 @@ def vatp_workspace_bytes(p: Params) -> int:
     return int(lib.vatp_workspace_bytes(C.byref(p)))
 
 
-class Cache:
-    """Device arrays of the decode state (allocated with torch, owned by this object)."""
+class _State:
+    """The per-slot and per-unit arrays that both forms of the decode state have."""
 
-    def __init__(self, p: Params, device="cuda"):
-        b, h, d, cap = p.batch, (p.kv_heads or p.heads), p.head_dim, int(lib.vatp_cache_capacity(p.budget))
-        dt = torch.float32 if p.dtype == F32 else torch.bfloat16
-        self.cap = cap
-        self.k_cache = torch.zeros(b, h, cap, d, dtype=dt, device=device)
-        self.v_cache = torch.zeros(b, h, cap, d, dtype=dt, device=device)
+    def __init__(self, p: Params, device, share):
+        b, h, cap = p.batch, (p.kv_heads or p.heads), int(lib.vatp_cache_capacity(p.budget))
+        self.cap, self.budget, self.batch = cap, p.budget, b
+        if share is not None:
+            if (share.cap, share.budget, share.pos.shape[:2]) != (cap, p.budget, (b, h)) or (share.ring is not None) != (p.indicator == IND_WINDOW) \
+                    or (share.ring is not None and share.ring.shape[2] != p.window_w):
+                raise ValueError("share: a state of other parameters")
+            for name in ("acc", "vnorm", "pos", "len", "free_slot", "next_pos", "last_slot", "ring", "acc_fixed"):
+                setattr(self, name, getattr(share, name))
+            return
         self.acc = torch.zeros(b, h, cap, dtype=torch.float32, device=device)
         self.vnorm = torch.zeros(b, h, cap, dtype=torch.float32, device=device)
         self.pos = torch.full((b, h, cap), -1, dtype=torch.int32, device=device)
@@ -137,12 +160,42 @@ class Cache:
         if p.indicator == IND_WINDOW:
             self.ring = torch.zeros(b, h, p.window_w, cap, dtype=torch.float32, device=device)
             self.acc_fixed = torch.zeros(b, h, cap, dtype=torch.int64, device=device)
-        self.struct = CacheStruct(*[_ptr(t) for t in (self.k_cache, self.v_cache, self.acc, self.vnorm, self.pos,
-                                                       self.len, self.free_slot, self.next_pos, self.ring,
-                                                       self.acc_fixed, self.last_slot)])
+
+    def _struct(self, k, v):
+        return CacheStruct(*[_ptr(t) for t in (k, v, self.acc, self.vnorm, self.pos, self.len, self.free_slot, self.next_pos, self.ring,
+                                               self.acc_fixed, self.last_slot)])
+
+
+class Cache(_State):
+    """Device arrays of the decode state (allocated with torch, owned by this object).  share: a state of the same parameters
+    (the 4-bit form of the same rows) whose arrays other than the rows this one uses too."""
+
+    def __init__(self, p: Params, device="cuda", share=None):
+        super().__init__(p, device, share)
+        b, h, d = p.batch, (p.kv_heads or p.heads), p.head_dim
+        dt = torch.float32 if p.dtype == F32 else torch.bfloat16
+        self.k_cache = torch.zeros(b, h, self.cap, d, dtype=dt, device=device)
+        self.v_cache = torch.zeros(b, h, self.cap, d, dtype=dt, device=device)
+        self.struct = self._struct(self.k_cache, self.v_cache)
 
     def nbytes(self) -> int:
         return sum(t.numel() * t.element_size() for t in (self.k_cache, self.v_cache, self.acc, self.vnorm, self.pos))
+
+
+class CacheQ4(_State):
+    """The decode state with K and V rows in 4 bits (vatp_cache_q4 in include/vatp.h has the format): codes [.., cap, head_dim / 2] uint8
+    and params [.., cap, head_dim / 32, 2] bf16 (scale, low end).  share: as for Cache."""
+
+    def __init__(self, p: Params, device="cuda", share=None):
+        super().__init__(p, device, share)
+        b, h, d = p.batch, (p.kv_heads or p.heads), p.head_dim
+        for name in ("k", "v"):
+            setattr(self, name + "_codes", torch.zeros(b, h, self.cap, d // 2, dtype=torch.uint8, device=device))
+            setattr(self, name + "_params", torch.zeros(b, h, self.cap, d // 32, 2, dtype=torch.bfloat16, device=device))
+        self.struct = CacheQ4Struct(self._struct(self.k_codes, self.v_codes), _ptr(self.k_params), _ptr(self.v_params))
+
+    def nbytes(self) -> int:
+        return sum(t.numel() * t.element_size() for t in (self.k_codes, self.v_codes, self.k_params, self.v_params, self.acc, self.vnorm, self.pos))
 
 
 def vatp_prefill_scores(p: Params, q, k, v, *, lse_out=None, attn_acc, vnorm, score, win_rows=None,
@@ -208,6 +261,40 @@ def vatp_decode_step(p: Params, cache: Cache, q_new, k_new, v_new, out, *, evict
                      stream=None):
     _check(lib.vatp_decode_step(C.byref(p), C.byref(cache.struct), _ptr(q_new), _ptr(k_new), _ptr(v_new), _ptr(out),
                                 _ptr(evicted_pos), _ptr(dev_status), _stream(stream)), "vatp_decode_step")
+
+
+def vatp_compact_q4(p: Params, k, v, attn_acc, vnorm, kept_idx, cache: CacheQ4, *, win_rows=None, dev_status=None, stream=None):
+    """vatp_compact into the 4-bit state."""
+    _check(lib.vatp_compact_q4(C.byref(p), _ptr(k), _ptr(v), _ptr(attn_acc), _ptr(vnorm), _ptr(win_rows), _ptr(kept_idx),
+                               C.byref(cache.struct), _ptr(dev_status), _stream(stream)), "vatp_compact_q4")
+
+
+def vatp_cache_pack_q4(p: Params, src: Cache, dst: CacheQ4, *, dev_status=None, stream=None):
+    """A decode state into one with 4-bit rows; arrays that both share stay as they are."""
+    _check(lib.vatp_cache_pack_q4(C.byref(p), C.byref(src.struct), C.byref(dst.struct), _ptr(dev_status), _stream(stream)),
+           "vatp_cache_pack_q4")
+
+
+def vatp_cache_unpack_q4(p: Params, src: CacheQ4, dst: Cache, *, dev_status=None, stream=None):
+    """The reverse: rows become the values that their codes stand for, rounded to the params dtype."""
+    _check(lib.vatp_cache_unpack_q4(C.byref(p), C.byref(src.struct), C.byref(dst.struct), _ptr(dev_status), _stream(stream)),
+           "vatp_cache_unpack_q4")
+
+
+def vatp_decode_step_q4(p: Params, cache: CacheQ4, q_new, k_new, v_new, out, *, evicted_pos=None, dev_status=None, stream=None):
+    """vatp_decode_step on the 4-bit state."""
+    _check(lib.vatp_decode_step_q4(C.byref(p), C.byref(cache.struct), _ptr(q_new), _ptr(k_new), _ptr(v_new), _ptr(out),
+                                   _ptr(evicted_pos), _ptr(dev_status), _stream(stream)), "vatp_decode_step_q4")
+
+
+def vatp_cache_copy(p: Params, src, dst, src_of, *, dev_status=None, stream=None):
+    """Entry b of `dst` (which p describes) becomes entry src_of[b] of `src`; SEQ_KEEP leaves it, SEQ_FREE empties it.  src_of: int32
+    [p.batch] on the device; both states Cache (vatp_cache_copy) or both CacheQ4 (vatp_cache_copy_q4)."""
+    if type(src) is not type(dst):
+        raise TypeError("both states must hold their rows in the same form")
+    name = "vatp_cache_copy_q4" if isinstance(dst, CacheQ4) else "vatp_cache_copy"
+    _check(getattr(lib, name)(C.byref(p), C.byref(src.struct), src.batch, src.budget, C.byref(dst.struct), _ptr(src_of), _ptr(dev_status),
+                              _stream(stream)), name)
 
 
 def vatp_selftest_bounded_wait(limit_ns: int, dev_status, waited_ns=None, *, stream=None):
