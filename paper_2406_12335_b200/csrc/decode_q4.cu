@@ -11,12 +11,18 @@
 //     head that the largest of them determines, and both are taken as a high fp16 half and a remainder (q of bf16 inputs has none);
 //   * rows are stored so that the 16 bytes a lane loads hold the channels it needs in an MMA operand, of every group: rows go from
 //     global memory into operand registers by plain 8- and 16-byte loads, without shared memory.
-// A unit is split over a thread-block cluster; the slots of a CTA over its eight warps, sixteen at a time.  A warp keeps its own
-// softmax (its maximum, sum and partial output; no barrier between the two products); the CTA joins them, the cluster joins the
-// CTAs' by st.async into the partners' shared memory, and every CTA then updates the indicators of its own slots and sends its
-// eviction candidate to rank 0.
+// A unit is split over a thread-block cluster; the slots of a CTA over eight warps, sixteen (a tile) at a time.
+//   * A tile of K or of V is 16 consecutive rows, two bulk copies (codes, parameters) into the warp's ring in shared memory.  As many
+//     as the ring holds are requested before the launch ahead has finished; the one row that it may have appended since (last_slot) is
+//     patched in.
+//   * A warp keeps its own softmax: its maximum, sum and partial output, without a barrier between the two products.
+//   * A ninth warp takes the incoming token, which is no part of any tile: it quantises and stores the rows and is a ninth partial.
+//   * The CTA joins its partials, the cluster those of its CTAs by st.async into the partners' shared memory; every CTA then updates the
+//     indicators of its own slots, and every warp sends its eviction candidate to rank 0.
 #include <cooperative_groups.h>
 #include <cuda_fp16.h>
+
+#include <type_traits>
 
 #include "q4.cuh"
 
@@ -25,38 +31,46 @@ namespace cg = cooperative_groups;
 namespace vatp {
 namespace {
 
-constexpr int Q4_WARPS = 8, Q4_THREADS = Q4_WARPS * 32;
+constexpr int Q4_WARPS = 8;            // that take slots
+constexpr int Q4_WORKERS = Q4_WARPS * 32, Q4_THREADS = Q4_WORKERS + 32;
 constexpr int Q4_TILE = 16;            // slots of a warp at a time
 constexpr int Q4_SPLIT = 8;            // CTAs of a unit at most
 constexpr int Q4_HEADS = 8;            // query heads of a unit at most (columns of the MMA tiles)
-constexpr int Q4_AHEAD = 2;            // tiles in flight per warp
+constexpr int Q4_DEPTH = 16;           // tiles in a warp's ring at most
 constexpr float Q4_LOG2E = 1.4426950408889634f;
 constexpr unsigned long long Q4_NO_KEY = ~0ull;
 
 __device__ __forceinline__ uint32_t s32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-__device__ __forceinline__ void bar_init(uint64_t* bar) { asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(s32(bar)) : "memory"); }
+__device__ __forceinline__ void bar_init(uint64_t* bar, uint32_t count) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(s32(bar)), "r"(count) : "memory");
+}
 __device__ __forceinline__ void bar_expect(uint64_t* bar, uint32_t bytes) {
   asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(s32(bar)), "r"(bytes) : "memory");
 }
-__device__ __forceinline__ bool bar_try(uint64_t* bar) {
+__device__ __forceinline__ bool bar_try(uint64_t* bar, uint32_t parity) {
   uint32_t ok;
   asm volatile(
       "{\n\t.reg .pred p;\n\t"
-      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], 0;\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
       "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok) : "r"(s32(bar)) : "memory");
+      : "=r"(ok) : "r"(s32(bar)), "r"(parity) : "memory");
   return ok != 0;
 }
-// bounded wait (about a second) for the barrier's first phase: false when what it counts never arrived
-__device__ __forceinline__ bool bar_wait(uint64_t* bar) {
-  if (bar_try(bar)) return true;
+// bounded wait (about a second): false when what the barrier counts never arrived
+__device__ __forceinline__ bool bar_wait(uint64_t* bar, uint32_t parity) {
+  if (bar_try(bar, parity)) return true;
   uint64_t t0, t1;
   asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t0));
-  while (!bar_try(bar)) {
+  while (!bar_try(bar, parity)) {
     asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t1));
     if (t1 - t0 > 1000000000ull) return false;
   }
   return true;
+}
+// global -> shared bulk copy; dst, src and bytes are multiples of 16
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint64_t* bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+               ::"r"(dst), "l"(src), "r"(bytes), "r"(s32(bar)) : "memory");
 }
 // address of `addr` (this CTA's shared memory) in CTA `rank` of the cluster
 __device__ __forceinline__ uint32_t at_rank(uint32_t addr, int rank) {
@@ -77,7 +91,7 @@ __device__ __forceinline__ void send4(uint32_t addr, uint32_t a, uint32_t b, uin
 }
 // D (16x8, fp32) += A (16x16, fp16, row) * B (16x8, fp16, col)
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
@@ -90,37 +104,22 @@ __device__ __forceinline__ uint32_t half2_of(float lo, float hi) {
   const __half2 h = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&h);
 }
-// Rows are read once, past L1: a step may request rows before its predecessor has finished, and what it requests again afterwards
-// must come from L2.
-__device__ __forceinline__ uint32_t load_row(const uint32_t* p) {
+// past L1: what the launch ahead has stored since this CTA requested the row early
+__device__ __forceinline__ uint32_t load_fresh(const uint32_t* p) {
   uint32_t x;
   asm volatile("ld.global.cg.u32 %0, [%1];" : "=r"(x) : "l"(p));
   return x;
 }
-__device__ __forceinline__ uint2 load_row(const uint2* p) {
-  uint2 x;
-  asm volatile("ld.global.cg.v2.u32 {%0, %1}, [%2];" : "=r"(x.x), "=r"(x.y) : "l"(p));
-  return x;
-}
-__device__ __forceinline__ uint4 load_row(const uint4* p) {
-  uint4 x;
-  asm volatile("ld.global.cg.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "l"(p));
-  return x;
-}
-template <int N> __device__ __forceinline__ void load_words(const void* p, uint32_t (&w)[N]) {
+template <int N> __device__ __forceinline__ void words_of(const unsigned char* p, uint32_t (&w)[N]) {      // from shared memory
   if constexpr (N == 1) {
-    w[0] = load_row(static_cast<const uint32_t*>(p));
+    w[0] = *reinterpret_cast<const uint32_t*>(p);
   } else if constexpr (N == 2) {
-    const uint2 x = load_row(static_cast<const uint2*>(p));
+    const uint2 x = *reinterpret_cast<const uint2*>(p);
     w[0] = x.x; w[1] = x.y;
   } else {
-    const uint4 x = load_row(static_cast<const uint4*>(p));
+    const uint4 x = *reinterpret_cast<const uint4*>(p);
     w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w;
   }
-}
-template <int N> __device__ __forceinline__ void copy_words(const unsigned char* p, uint32_t (&w)[N]) {
-#pragma unroll
-  for (int i = 0; i < N; ++i) w[i] = reinterpret_cast<const uint32_t*>(p)[i];
 }
 
 // eight or four consecutive channels of a new row
@@ -165,29 +164,34 @@ __device__ __forceinline__ unsigned long long min_key(unsigned long long key) {
 
 // GT: 1 - one query head per cache; 4 - two to four, the columns of the second product are the heads' high halves and then the
 // remainders; 8 - five to eight, a column a head and two products.
-// Dynamic shared memory: partial outputs of the warps [8][G][HD] | logits [G][ld].
+// Dynamic shared memory: rings [8][depth][tile], which take the warps' partial outputs in the end | the ninth partial [G][HD] |
+// logits [G][chunk].
+template <int HD> constexpr int q4_item = Q4_TILE * (HD / 2 + HD / 8);      // bytes of a tile: codes, then parameters
+
 template <typename T, int HD, bool WINDOWED, int GT>
 __global__ void __launch_bounds__(Q4_THREADS, 2)
-decode_q4_kernel(int G_arg, int split, int chunk, int ld, int B, int cap, int F, int R, int w, int norm, float scale_log2, vatp_cache_q4 c, const T* q_new,
+decode_q4_kernel(int G_arg, int split, int chunk, int depth, int B, int cap, int F, int R, int w, int norm, float scale_log2, vatp_cache_q4 c, const T* q_new,
                  const T* k_new, const T* v_new, T* out, int32_t* evicted, int32_t* dev_status) {
   constexpr int NG = HD / 32, KW = HD / 32, VW = HD / 64;       // groups of a row; 32-bit words of a lane in a K row and a V row
   constexpr int KP = GT == 1 ? 1 : NG;                          // parameter words of a lane per K row
+  constexpr int CODES = HD / 2, PARAMS = NG * 4, ITEM = q4_item<HD>;      // bytes of a row's codes and parameters, of a tile
   constexpr bool SPLIT_Q = sizeof(T) == 4;                      // q has a remainder beyond its high half
+  constexpr int XC = GT > 4 ? 16 : 8;                           // columns of the second product's operand: see x_col
+  constexpr int NT = GT > 4 ? 1 : 2;                            // tiles a warp works on at a time (with eight heads: registers)
   const int G = GT == 1 ? 1 : G_arg;
-  extern __shared__ float dyn[];
-  float* part_o = dyn;
-  float* logit_s = dyn + Q4_WARPS * G * HD;
-  constexpr int XC = GT > 4 ? 16 : 8, X_LOW = XC / 2;           // columns of the second product's operand; the remainders' first one
-  __shared__ __align__(16) uint16_t xs[Q4_WARPS][NG][XC][Q4_TILE];     // [group][column][slot]
-  __shared__ __align__(16) unsigned char new_row[2][HD / 2 + 4 * NG];  // the incoming token's K and V row: codes, parameters
-  __shared__ float part_m[Q4_WARPS][GT], part_j[Q4_WARPS][GT], part_l[Q4_WARPS][GT], part_lo[Q4_WARPS][GT][NG];
-  __shared__ float f_m[Q4_WARPS][GT], f_j[Q4_WARPS][GT];      // the warps' factors towards the CTA's maximum
-  __shared__ float xo[GT * HD];                                        // slices of partial outputs received [split][G][HD / split]
-  __shared__ float2 ex_ml[Q4_SPLIT][GT];                               // per rank and head: maximum of its logits, sum of exp2(s - m)
+  // high half and remainder of head h: neighbours, i.e. in one lane's accumulators, or eight columns apart (two products)
+  auto x_col = [](int h, int low) { return GT > 4 ? h + 8 * low : 2 * h + low; };
+  extern __shared__ __align__(128) unsigned char dyn[];
+  const int ring_bytes = depth * ITEM;                          // of a warp
+  float* new_o = reinterpret_cast<float*>(dyn + Q4_WARPS * ring_bytes);
+  float* logit_s = new_o + G * HD;
+  __shared__ __align__(16) uint16_t xs[Q4_WARPS][NT][NG][XC][Q4_TILE];      // [tile][group][column][slot: 4 (slot mod 4) + slot / 4]
+  __shared__ float part_m[Q4_WARPS + 1][GT], part_l[Q4_WARPS + 1][GT], part_lo[Q4_WARPS][GT][NG];
+  __shared__ float xo[GT * HD];                                         // slices of partial outputs received [split][G][HD / split]
+  __shared__ float2 ex_ml[Q4_SPLIT][GT];                                // per rank and head: maximum of its logits, sum of exp2(s - m)
   __shared__ float fr_s[Q4_SPLIT][GT], all_m[GT], all_inv[GT], new_norm_s;
-  __shared__ Q4Candidate cand[Q4_SPLIT];
-  __shared__ unsigned long long warp_key[Q4_WARPS];
-  __shared__ __align__(8) uint64_t ex_bar, cand_bar;
+  __shared__ Q4Candidate cand[Q4_SPLIT * Q4_WARPS];                     // in rank 0
+  __shared__ __align__(8) uint64_t full[Q4_WARPS][Q4_DEPTH], k_done, ex_bar, cand_bar;
 
   const int rank = split > 1 ? (int)cg::this_cluster().block_rank() : 0;
   const int tid = threadIdx.x, lane = tid & 31, wid = __shfl_sync(0xffffffffu, tid >> 5, 0);
@@ -195,353 +199,137 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int B, int cap, int F,
   const int u = blockIdx.x / split;
   const int s0 = min(rank * chunk, cap), rows_alloc = min(chunk, cap - s0);      // this CTA's slots of the unit
   const int64_t base = (int64_t)u * cap + s0;
-  if (tid == 0) {
-    bar_init(&ex_bar);
-    bar_init(&cand_bar);
-    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    if (split > 1) {
-      bar_expect(&ex_bar, (uint32_t)(8 * G * split + 4 * G * HD));
-      if (rank == 0) bar_expect(&cand_bar, (uint32_t)(split * sizeof(Q4Candidate)));
-    }
+  if (tid < Q4_WARPS * Q4_DEPTH) bar_init(&full[0][tid], 1);
+  if (tid == Q4_WORKERS) {
+    bar_init(&k_done, Q4_WARPS + 1);
+    bar_init(&ex_bar, 1);
+    bar_init(&cand_bar, 1);
   }
-  for (int i = lane; i < NG * XC * Q4_TILE / 2; i += 32) reinterpret_cast<uint32_t*>(xs[wid])[i] = 0u;      // (columns without a head stay 0)
+  asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  if (tid == Q4_WORKERS) {
+    bar_expect(&ex_bar, (uint32_t)(8 * G * split + 4 * G * HD));
+    if (rank == 0) bar_expect(&cand_bar, (uint32_t)(split * Q4_WARPS * sizeof(Q4Candidate)));
+  }
+  if (wid < Q4_WARPS)      // (columns without a head stay 0)
+    for (int i = lane; i < NT * NG * XC * Q4_TILE / 2; i += 32) reinterpret_cast<uint32_t*>(xs[wid])[i] = 0u;
   __syncthreads();
+  // Another CTA's shared memory may only be written once that CTA runs and its barriers are armed: everyone arrives here and
+  // waits (long since satisfied) just before the first remote store.
   if (split > 1) cluster_arrive_release();
 
-  // ---- a tile's rows: K rows r8 and r8 + 8 with the channels of chunks 2 t4 and 2 t4 + 1, V rows 4 t4 .. + 3 with those of chunk r8
-  const unsigned char* kc = static_cast<const unsigned char*>(c.state.k_cache) + base * (HD / 2);
-  const unsigned char* vc = static_cast<const unsigned char*>(c.state.v_cache) + base * (HD / 2);
-  const uint32_t* kp = static_cast<const uint32_t*>(c.k_params) + base * NG;
-  const uint32_t* vp = static_cast<const uint32_t*>(c.v_params) + base * NG;
-  struct KTile { uint32_t w[2][KW], p[2][KP], v[2]; };      // v: V's parameters of group t4, for the bound on p sc
-  struct VTile { uint32_t w[4][VW], p[VW]; };               // p: parameters of slot lane / 2, groups VW (lane mod 2) ..
-  auto load_k = [&](KTile& x, int r0) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int row = min(r0 + r8 + 8 * i, rows_alloc - 1);      // (rows beyond the last are not used)
-      load_words(kc + (int64_t)row * (HD / 2) + t4 * (HD / 8), x.w[i]);
-      if constexpr (GT == 1) x.p[i][0] = t4 < NG ? load_row(kp + (int64_t)row * NG + t4) : 0u;
-      else load_words(kp + (int64_t)row * NG, x.p[i]);
-      x.v[i] = t4 < NG ? load_row(vp + (int64_t)row * NG + t4) : 0u;
-    }
+  bool bad = false;                      // this thread's wait ran out: it no longer waits, the results are void
+  const unsigned char* kc = static_cast<const unsigned char*>(c.state.k_cache) + base * CODES;
+  const unsigned char* vc = static_cast<const unsigned char*>(c.state.v_cache) + base * CODES;
+  const unsigned char* kp = static_cast<const unsigned char*>(c.k_params) + base * PARAMS;
+  const unsigned char* vp = static_cast<const unsigned char*>(c.v_params) + base * PARAMS;
+  unsigned char* ring = dyn + (size_t)wid * ring_bytes;
+  // This warp's tiles: wid, wid + 8, ...; n of them among the first `rows` slots.  Item j < n of its ring is the j-th tile of K,
+  // item n + j of V.
+  auto tiles_in = [&](int rows) { return wid * Q4_TILE < rows ? (rows - wid * Q4_TILE + Q4_WARPS * Q4_TILE - 1) / (Q4_WARPS * Q4_TILE) : 0; };
+  auto tile_row = [&](int j) { return (wid + Q4_WARPS * j) * Q4_TILE; };
+  auto request = [&](int j, int n, int slot) {      // one lane: item j into ring slot `slot`
+    const int r0 = tile_row(j < n ? j : j - n), rows = min(Q4_TILE, rows_alloc - r0);      // (8 or 16)
+    uint64_t* bar = &full[wid][slot];
+    bar_expect(bar, (uint32_t)(rows * (CODES + PARAMS)));
+    const uint32_t dst = s32(ring) + slot * ITEM;
+    bulk_load(dst, (j < n ? kc : vc) + (int64_t)r0 * CODES, rows * CODES, bar);
+    bulk_load(dst + Q4_TILE * CODES, (j < n ? kp : vp) + (int64_t)r0 * PARAMS, rows * PARAMS, bar);
   };
-  auto load_v = [&](VTile& x, int r0) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) load_words(vc + (int64_t)min(r0 + 4 * t4 + i, rows_alloc - 1) * (HD / 2) + r8 * (HD / 16), x.w[i]);
-    load_words(vp + (int64_t)min(r0 + (lane >> 1), rows_alloc - 1) * NG + (lane & 1) * VW, x.p);
-  };
-  constexpr int RSTEP = Q4_WARPS * Q4_TILE;
-  const int first = wid * Q4_TILE;
-  KTile kt[Q4_AHEAD];
-#pragma unroll
-  for (int a = 0; a < Q4_AHEAD; ++a)
-    if (first + a * RSTEP < rows_alloc) load_k(kt[a], first + a * RSTEP);
-  // Nothing but K and V rows is read before the previous launch has completed.
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  const int len = min(max(c.state.len[u], 0), cap - 1), fs = min(max(c.state.free_slot[u], 0), cap - 1);
-  const int t = c.state.next_pos[u], ls = c.state.last_slot[u];
-  const int hi = len + 1;                // slots [0, hi) are live once the new token is in
-  const int cnt = max(min(hi - s0, rows_alloc), 0);
-  const int fs_local = fs - s0;
-  const bool owns_new = fs_local >= 0 && fs_local < cnt;
-  const int new_warp = owns_new ? (fs_local / Q4_TILE) % Q4_WARPS : -1;
-  // The row that the previous step appended may have been requested before it was stored.
-  const int ls_local = ls - s0;
-#pragma unroll
-  for (int a = 0; a < Q4_AHEAD; ++a) {
-    const int r0 = first + a * RSTEP;
-    if (ls >= 0 && r0 < rows_alloc && ls_local >= r0 && ls_local < r0 + Q4_TILE) load_k(kt[a], r0);
-  }
-  VTile vt[Q4_AHEAD];
-#pragma unroll
-  for (int a = 0; a < Q4_AHEAD; ++a)
-    if (first + a * RSTEP < cnt) load_v(vt[a], first + a * RSTEP);
-
-  // ---- B operand of K q^T.  Lane (n = r8, t4): channels 8 t4 .. 8 t4 + 7 of every group of its column's head.
-  // GT == 1: column 2 g carries the high half of group g alone, column 2 g + 1 its remainder: every lane of a row's four then
-  // holds one group's sum, to be scaled by that group's parameters.  Else: column n is head n.
-  uint32_t qb[NG][4], qr[GT > 1 && SPLIT_Q ? NG : 1][4];
-  float q_back, qsum[GT > 1 ? NG : 1][2];      // 2^24 / (the head's power of two) * scale; sums of q over groups, * scale
-  {
-    const T* qp = q_new + ((int64_t)u * G + (GT == 1 ? 0 : min(r8, G - 1))) * HD + 8 * t4;
-    float q[NG][8], most = 0.f;
-#pragma unroll
-    for (int g = 0; g < NG; ++g)
-      load_new(qp + 32 * g, q[g]);
-#pragma unroll
-    for (int g = 0; g < NG; ++g)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(q[g][e]));
-    most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
-    most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
-    // power of two that brings the largest to [2^13, 2^14)
-    const int ex = min(max(13 + 127 - (int)(__float_as_uint(most) >> 23), -100), 126);
-    const float up = __uint_as_float((uint32_t)(ex + 127) << 23), back = __uint_as_float((uint32_t)(24 - ex + 127) << 23) * scale_log2;
-    float gs[NG];
-#pragma unroll
-    for (int g = 0; g < NG; ++g) {
-      float s = 0.f;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) s += q[g][e];
-      s += __shfl_xor_sync(0xffffffffu, s, 1);
-      s += __shfl_xor_sync(0xffffffffu, s, 2);
-      gs[g] = s * scale_log2;
-      float a[8], rest[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float x = q[g][e] * (e & 1 ? up * 0.0625f : up);      // (odd channels' codes stand four bits higher)
-        a[e] = __half2float(__float2half_rn(x));
-        rest[e] = x - a[e];
-      }
-      const bool low = GT == 1 && SPLIT_Q && (r8 & 1), mine = GT > 1 || (r8 >> 1) == g;
-      if (GT == 1 && !SPLIT_Q && (r8 & 1)) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) a[e] = 0.f;
-      }
-#pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        qb[g][x] = mine ? (low ? half2_of(rest[x], rest[x + 4]) : half2_of(a[x], a[x + 4])) : 0u;
-        if constexpr (GT > 1 && SPLIT_Q) qr[g][x] = half2_of(rest[x], rest[x + 4]);
-      }
-    }
-    if constexpr (GT == 1) {
-      q_back = back;
-      float s = gs[0];
-#pragma unroll
-      for (int g = 1; g < NG; ++g) s = t4 == g ? gs[g] : s;
-      qsum[0][0] = t4 < NG ? s : 0.f;
-      qsum[0][1] = 0.f;
-    } else {
-      // (an accumulator's columns are heads 2 t4 and 2 t4 + 1; their sums are with the lanes of those columns)
-#pragma unroll
-      for (int g = 0; g < NG; ++g)
-#pragma unroll
-        for (int x = 0; x < 2; ++x) qsum[g][x] = __shfl_sync(0xffffffffu, gs[g], 4 * (2 * t4 + x));
-      q_back = back;
-    }
-  }
-  float q_back2[2];
-  if constexpr (GT > 1) {
-#pragma unroll
-    for (int x = 0; x < 2; ++x) q_back2[x] = __shfl_sync(0xffffffffu, q_back, 4 * (2 * t4 + x));
-  }
-
-  // ---- the incoming token: quantised, stored, and kept for the tiles that hold its slot; its norm (Eq. 4)
-  if (wid == new_warp) {
-    float norm_v = 0.f;
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      float y[4] = {0.f, 0.f, 0.f, 0.f};
-      if (lane < HD / 4) load_new((x ? v_new : k_new) + (int64_t)u * HD + 4 * lane, y);
-      uint32_t par;
-      const uint32_t code = q4_row(y, par);
-      if (lane < HD / 4) {
-        *reinterpret_cast<uint16_t*>(new_row[x] + q4_byte<HD>(lane >> 3, lane & 7)) = (uint16_t)code;
-        if ((lane & 7) == 0) reinterpret_cast<uint32_t*>(new_row[x] + HD / 2)[lane >> 3] = par;
-      }
-      if (x) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) norm_v = norm_fold(norm, norm_v, y[e]);
-#pragma unroll
-        for (int o = 16; o; o >>= 1) norm_v = norm_merge(norm, norm_v, __shfl_xor_sync(0xffffffffu, norm_v, o));
-        norm_v = norm_finish(norm, norm_v);
-      }
-    }
-    __syncwarp();
-    constexpr int CW = HD / 8;             // words of a row's codes
-    const int x = lane >> 4, i = lane & 15;
-    const uint32_t* from = reinterpret_cast<const uint32_t*>(new_row[x]);
-    if (i < CW) reinterpret_cast<uint32_t*>(static_cast<unsigned char*>(x ? c.state.v_cache : c.state.k_cache) + (base + fs_local) * (HD / 2))[i] = from[i];
-    if (i < NG) static_cast<uint32_t*>(x ? c.v_params : c.k_params)[(base + fs_local) * NG + i] = from[CW + i];
-    if (lane == 0) {
-      new_norm_s = norm_v;
-      c.state.vnorm[base + fs_local] = norm_v;
-      c.state.pos[base + fs_local] = t;
-    }
-  }
-
-  // ---- logits of this warp's tiles, their maximum and that of s + log2 sc_v (J, rounded up: what p sc may amount to)
-  constexpr int MX = GT > 1 ? 2 : 1;
-  float m_run[MX], j_run[MX];
-#pragma unroll
-  for (int x = 0; x < MX; ++x) m_run[x] = j_run[x] = -INFINITY;
-  for (int r0 = first; r0 < cnt; r0 += Q4_AHEAD * RSTEP) {
-#pragma unroll
-    for (int a = 0; a < Q4_AHEAD; ++a) {
-      const int rt = r0 + a * RSTEP;
-      if (rt >= cnt) break;
-      KTile& k = kt[a];
-      if (wid == new_warp && fs_local >= rt && fs_local < rt + Q4_TILE) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-          if (rt + r8 + 8 * i == fs_local) {
-            copy_words(new_row[0] + t4 * (HD / 8), k.w[i]);
-            copy_words(new_row[0] + HD / 2 + (GT == 1 ? 4 * min(t4, NG - 1) : 0), k.p[i]);
-            if (GT == 1 && t4 >= NG) k.p[i][0] = 0u;
-            if (t4 < NG) k.v[i] = reinterpret_cast<const uint32_t*>(new_row[1] + HD / 2)[t4];
-          }
-      }
-      float acc[GT > 1 ? NG : 2][4];
-#pragma unroll
-      for (int g = 0; g < (GT > 1 ? NG : 2); ++g) acc[g][0] = acc[g][1] = acc[g][2] = acc[g][3] = 0.f;
-#pragma unroll
-      for (int g = 0; g < NG; ++g) {
-        // words of chunks 2 t4 (first half of the lane's words) and 2 t4 + 1; a half word is a group
-        const uint32_t sel = g & 1 ? 0x7632u : 0x5410u;
-        const uint32_t xa = __byte_perm(k.w[0][g >> 1], k.w[0][KW / 2 + (g >> 1)], sel);
-        const uint32_t xb = __byte_perm(k.w[1][g >> 1], k.w[1][KW / 2 + (g >> 1)], sel);
-        float(&d0)[4] = acc[GT > 1 ? g : 0];
-        float(&d1)[4] = acc[GT > 1 ? g : 1];
-        mma_f16(d0, xa & 0x000f000fu, xb & 0x000f000fu, xa & 0x00f000f0u, xb & 0x00f000f0u, qb[g][0], qb[g][1]);
-        mma_f16(d1, xa >> 8 & 0x000f000fu, xb >> 8 & 0x000f000fu, xa >> 8 & 0x00f000f0u, xb >> 8 & 0x00f000f0u, qb[g][2], qb[g][3]);
-        if constexpr (GT > 1 && SPLIT_Q) {
-          mma_f16(d0, xa & 0x000f000fu, xb & 0x000f000fu, xa & 0x00f000f0u, xb & 0x00f000f0u, qr[g][0], qr[g][1]);
-          mma_f16(d1, xa >> 8 & 0x000f000fu, xb >> 8 & 0x000f000fu, xa >> 8 & 0x00f000f0u, xb >> 8 & 0x00f000f0u, qr[g][2], qr[g][3]);
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int row = rt + r8 + 8 * i;
-        const bool live = row < cnt;
-        float s[MX];
-        if constexpr (GT == 1) {
-          const float d = (acc[0][2 * i] + acc[1][2 * i]) + (acc[0][2 * i + 1] + acc[1][2 * i + 1]);
-          s[0] = fmaf(q4_scale(k.p[i][0]) * q_back, d, q4_low(k.p[i][0]) * qsum[0][0]);
-          s[0] += __shfl_xor_sync(0xffffffffu, s[0], 1);
-          s[0] += __shfl_xor_sync(0xffffffffu, s[0], 2);
-        } else {
-#pragma unroll
-          for (int x = 0; x < 2; ++x) {
-            float d = 0.f, l = 0.f;
-#pragma unroll
-            for (int g = 0; g < NG; ++g) {
-              d = fmaf(q4_scale(k.p[i][g]), acc[g][2 * i + x], d);
-              l = fmaf(q4_low(k.p[i][g]), qsum[g][x], l);
-            }
-            s[x] = fmaf(d, q_back2[x], l);
-          }
-        }
-        // exponent of the largest scale of V's row, rounded up
-        int ev = max((int)(k.v[i] >> 7 & 0xffu) - 126, -100);
-        ev = max(ev, __shfl_xor_sync(0xffffffffu, ev, 1));
-        ev = max(ev, __shfl_xor_sync(0xffffffffu, ev, 2));
-#pragma unroll
-        for (int x = 0; x < MX; ++x) {
-          if (!live) s[x] = -INFINITY;
-          const int h = GT > 1 ? 2 * t4 + x : 0;
-          if (GT > 1 ? h < G : t4 == 0) logit_s[h * ld + row] = s[x];
-          m_run[x] = fmaxf(m_run[x], s[x]);
-          j_run[x] = fmaxf(j_run[x], s[x] + (float)ev);
-        }
-      }
-      if (rt + Q4_AHEAD * RSTEP < cnt) load_k(kt[a], rt + Q4_AHEAD * RSTEP);
-    }
-  }
-  // (after the wait: at most one unfinished predecessor exists while a successor sets up)
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-#pragma unroll
-  for (int x = 0; x < MX; ++x) {
-#pragma unroll
-    for (int o = 4; o < 32; o <<= 1) {
-      m_run[x] = fmaxf(m_run[x], __shfl_xor_sync(0xffffffffu, m_run[x], o));
-      j_run[x] = fmaxf(j_run[x], __shfl_xor_sync(0xffffffffu, j_run[x], o));
-    }
-    const int h = GT > 1 ? 2 * t4 + x : 0;
-    if (r8 == 0 && (GT > 1 ? h < G : t4 == 0)) { part_m[wid][h] = m_run[x]; part_j[wid][h] = j_run[x]; }
-  }
+  const int n_alloc = wid < Q4_WARPS && rows_alloc > 0 ? tiles_in(rows_alloc) : 0, early = min(depth, 2 * n_alloc);
+  if (lane == 0)
+    for (int j = 0; j < early; ++j) request(j, n_alloc, j);
   __syncwarp();
 
-  // ---- O^T += V^T (p sc): A = codes (16 channels x 16 slots), B = p sc by slot and head
-  float o_acc[NG][2][4];
+  // Nothing but K and V rows is read before the previous launch has completed.
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int len_m = c.state.len[u], fs_m = c.state.free_slot[u], t = c.state.next_pos[u], ls = c.state.last_slot[u];
+
+  if (wid == Q4_WARPS) {
+    // ---- the ninth warp: the incoming token.  Lane l < HD / 4 has channels 4 l .. 4 l + 3.
+    float kv[2][4], qv[GT][4];
 #pragma unroll
-  for (int g = 0; g < NG; ++g)
+    for (int e = 0; e < 4; ++e) {
+      kv[0][e] = kv[1][e] = 0.f;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) o_acc[g][i][0] = o_acc[g][i][1] = o_acc[g][i][2] = o_acc[g][i][3] = 0.f;
-  float l_run[GT], lo_run[GT][VW];        // of this lane's slots (and groups): sum of p, sum of p lo
+      for (int h = 0; h < GT; ++h) qv[h][e] = 0.f;
+    }
+    if (lane < HD / 4) {
+      load_new(k_new + (int64_t)u * HD + 4 * lane, kv[0]);
+      load_new(v_new + (int64_t)u * HD + 4 * lane, kv[1]);
 #pragma unroll
-  for (int h = 0; h < GT; ++h) {
-    l_run[h] = 0.f;
+      for (int h = 0; h < GT; ++h)
+        if (h < G) load_new(q_new + ((int64_t)u * G + h) * HD + 4 * lane, qv[h]);
+    }
+    const int len = min(max(len_m, 0), cap - 1), fs_local = min(max(fs_m, 0), cap - 1) - s0;
+    const int cnt = max(min(len + 1 - s0, rows_alloc), 0);
+    const bool owns = fs_local >= 0 && fs_local < cnt;
+    float s[GT];
 #pragma unroll
-    for (int i = 0; i < VW; ++i) lo_run[h][i] = 0.f;
-  }
-  for (int r0 = first; r0 < cnt; r0 += Q4_AHEAD * RSTEP) {
+    for (int h = 0; h < GT; ++h) s[h] = -INFINITY;
+    if (owns) {
+      float nv = 0.f;
 #pragma unroll
-    for (int a = 0; a < Q4_AHEAD; ++a) {
-      const int rt = r0 + a * RSTEP;
-      if (rt >= cnt) break;
-      VTile& v = vt[a];
-      if (wid == new_warp && fs_local >= rt && fs_local < rt + Q4_TILE) {
+      for (int e = 0; e < 4; ++e) nv = norm_fold(norm, nv, kv[1][e]);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (rt + 4 * t4 + i == fs_local) copy_words(new_row[1] + r8 * (HD / 16), v.w[i]);
-        if (rt + (lane >> 1) == fs_local) copy_words(new_row[1] + HD / 2 + (lane & 1) * VW * 4, v.p);
+      for (int x = 0; x < 2; ++x) {
+        uint32_t par;
+        const uint32_t code = q4_row(kv[x], par);
+        if (lane < HD / 4 && VATP_INB(s0 + fs_local, cap, dev_status)) {
+          unsigned char* row = static_cast<unsigned char*>(x ? c.state.v_cache : c.state.k_cache) + (base + fs_local) * CODES;
+          *reinterpret_cast<uint16_t*>(row + q4_byte<HD>(lane >> 3, lane & 7)) = (uint16_t)code;
+          if ((lane & 7) == 0) static_cast<uint32_t*>(x ? c.v_params : c.k_params)[(base + fs_local) * NG + (lane >> 3)] = par;
+        }
+        // the values as stored
+#pragma unroll
+        for (int e = 0; e < 4; ++e) kv[x][e] = fmaf((float)(code >> (4 * e) & 15u), q4_scale(par), q4_low(par));
       }
-      const int slot = rt + (lane >> 1);
-      const bool live = slot < cnt;
 #pragma unroll
       for (int h = 0; h < GT; ++h) {
-        if (GT > 1 && h >= G) break;
-        const float s = logit_s[h * ld + slot];      // (-inf from cnt on)
-        const float p = live ? exp2_fast(s - part_m[wid][h]) : 0.f, y = live ? exp2_fast(s - part_j[wid][h] + 14.f) : 0.f;
-        l_run[h] += p;
+        if (GT > 1 && h >= G) continue;
+        float d = 0.f;
+        if (lane < HD / 4) {
 #pragma unroll
-        for (int i = 0; i < VW; ++i) {
-          const float x = live ? y * q4_scale(v.p[i]) : 0.f;
-          if (live) lo_run[h][i] = fmaf(p, q4_low(v.p[i]), lo_run[h][i]);
-          const __half hh = __float2half_rn(x), hl = __float2half_rn(x - __half2float(hh));
-          const int g = (lane & 1) * VW + i;
-          xs[wid][g][h][lane >> 1] = __half_as_ushort(hh);
-          xs[wid][g][h + X_LOW][lane >> 1] = __half_as_ushort(hl);
+          for (int e = 0; e < 4; ++e) d = fmaf(qv[h][e], kv[0][e], d);
         }
-      }
-      __syncwarp();
 #pragma unroll
-      for (int g = 0; g < NG; ++g) {
-        const uint2 b = *reinterpret_cast<const uint2*>(&xs[wid][g][r8][4 * t4]);
-        const uint32_t sel = g & 1 ? 0x7632u : 0x5410u;
-        const uint32_t xa = __byte_perm(v.w[0][g >> 1], v.w[1][g >> 1], sel), xb = __byte_perm(v.w[2][g >> 1], v.w[3][g >> 1], sel);
-        mma_f16(o_acc[g][0], xa & 0x000f000fu, xa & 0x00f000f0u, xb & 0x000f000fu, xb & 0x00f000f0u, b.x, b.y);
-        mma_f16(o_acc[g][1], xa >> 8 & 0x000f000fu, xa >> 8 & 0x00f000f0u, xb >> 8 & 0x000f000fu, xb >> 8 & 0x00f000f0u, b.x, b.y);
-        if constexpr (GT > 4) {
-          const uint2 d = *reinterpret_cast<const uint2*>(&xs[wid][g][X_LOW + r8][4 * t4]);
-          mma_f16(o_acc[g][0], xa & 0x000f000fu, xa & 0x00f000f0u, xb & 0x000f000fu, xb & 0x00f000f0u, d.x, d.y);
-          mma_f16(o_acc[g][1], xa >> 8 & 0x000f000fu, xa >> 8 & 0x00f000f0u, xb >> 8 & 0x000f000fu, xb >> 8 & 0x00f000f0u, d.x, d.y);
-        }
+        for (int o = 16; o; o >>= 1) d += __shfl_xor_sync(0xffffffffu, d, o);
+        s[h] = d * scale_log2;
+        if (lane == 0) logit_s[h * chunk + fs_local] = s[h];
       }
-      __syncwarp();
-      if (rt + Q4_AHEAD * RSTEP < cnt) load_v(vt[a], rt + Q4_AHEAD * RSTEP);
+#pragma unroll
+      for (int o = 16; o; o >>= 1) nv = norm_merge(norm, nv, __shfl_xor_sync(0xffffffffu, nv, o));
+      nv = norm_finish(norm, nv);
+      if (lane == 0) {
+        new_norm_s = nv;
+        c.state.vnorm[base + fs_local] = nv;
+        c.state.pos[base + fs_local] = t;
+      }
+    }
+    if (lane == 0) {
+#pragma unroll
+      for (int h = 0; h < GT; ++h)
+        if (GT == 1 || h < G) part_m[Q4_WARPS][h] = s[h];
+      asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(s32(&k_done)) : "memory");
+    }
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    if (!bar_wait(&k_done, 0)) bad = true;
+#pragma unroll
+    for (int h = 0; h < GT; ++h) {
+      if (GT > 1 && h >= G) continue;
+      float m = s[h];
+#pragma unroll
+      for (int k = 0; k < Q4_WARPS; ++k) m = fmaxf(m, part_m[k][h]);
+      const float f = owns ? exp2_fast(s[h] - m) : 0.f;
+      if (lane == 0) part_l[Q4_WARPS][h] = f;
+      if (lane < HD / 4) *reinterpret_cast<float4*>(new_o + h * HD + 4 * lane) = make_float4(kv[1][0] * f, kv[1][1] * f, kv[1][2] * f, kv[1][3] * f);
     }
   }
-  // ---- the warp's partial: sums of p (even lanes), of p lo, and O^T with its constant factors (codes in odd channels stand four
-  // bits higher)
-#pragma unroll
-  for (int h = 0; h < GT; ++h) {
-    if (GT > 1 && h >= G) break;
-#pragma unroll
-    for (int o = 2; o < 32; o <<= 1) {
-      l_run[h] += __shfl_xor_sync(0xffffffffu, l_run[h], o);
-#pragma unroll
-      for (int i = 0; i < VW; ++i) lo_run[h][i] += __shfl_xor_sync(0xffffffffu, lo_run[h][i], o);
-    }
-    if (lane < 2) {
-      if (lane == 0) part_l[wid][h] = l_run[h];
-#pragma unroll
-      for (int i = 0; i < VW; ++i) part_lo[wid][h][lane * VW + i] = lo_run[h][i];
-    }
-  }
-#pragma unroll
-  for (int g = 0; g < NG; ++g)
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        float o = o_acc[g][i][x];
-        if (GT <= 4) o += __shfl_xor_sync(0xffffffffu, o, 2);      // (the remainder's column)
-        const int h = 2 * t4 + (x & 1);
-        if (h < G) part_o[((size_t)wid * G + h) * HD + 32 * g + 4 * r8 + 2 * i + (x >> 1)] = x & 2 ? o * 0.0625f : o;
-      }
-  // ---- the state of this thread's slots tid, tid + 256, ...: the first ones read while the CTAs exchange
-  constexpr int SB = 2;
+
+  const int len = min(max(len_m, 0), cap - 1), fs = min(max(fs_m, 0), cap - 1);
+  const int hi = len + 1;                // slots [0, hi) are live once the new token is in
+  const int cnt = max(min(hi - s0, rows_alloc), 0);
+  const int fs_local = fs - s0, ls_local = ls - s0;
+  constexpr int SB = 2;                  // slots of a thread whose state is in registers at a time
   float old_r[SB], norm_r[SB];
   int pos_r[SB];
   long long fx_r[WINDOWED ? SB : 1];
@@ -549,7 +337,7 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int B, int cap, int F,
   auto fetch = [&](int i0) {
 #pragma unroll
     for (int k = 0; k < SB; ++k) {
-      const int i = i0 + k * Q4_THREADS;
+      const int i = i0 + k * Q4_WORKERS;
       old_r[k] = norm_r[k] = 0.f;
       pos_r[k] = 0;
       if (WINDOWED) fx_r[k] = 0;
@@ -561,49 +349,400 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int B, int cap, int F,
       }
     }
   };
-  fetch(tid);
-  __syncthreads();
-  if (tid < Q4_WARPS * G) {
-    const int k = tid / G, h = tid - k * G;
-    float m = part_m[0][h];
+
+  if (wid < Q4_WARPS) {
+    // ---- B operand of K q^T.  Lane (n = r8, t4): channels 8 t4 .. 8 t4 + 7 of every group of its column's head.
+    // GT == 1: column 2 g carries the high half of group g alone, column 2 g + 1 its remainder: every lane of a row's four then
+    // holds one group's sum, to be scaled by that group's parameters.  Else: column n is head n.
+    uint32_t qb[NG][4], qr[GT > 1 && SPLIT_Q ? NG : 1][4];
+    float q_back[GT > 1 ? 2 : 1], qsum[GT > 1 ? NG : 1][2];      // 2^24 / (the head's power of two) * scale; sums of q over groups, * scale
+    {
+      // (GT == 1: of group r8 / 2 alone)
+      constexpr int QG = GT == 1 ? 1 : NG;
+      const int g0 = GT == 1 ? min(r8 >> 1, NG - 1) : 0;
+      const T* qp = q_new + ((int64_t)u * G + (GT == 1 ? 0 : min(r8, G - 1))) * HD + 32 * g0 + 8 * t4;
+      float q[QG][8], most = 0.f, gs[QG];
 #pragma unroll
-    for (int i = 1; i < Q4_WARPS; ++i) m = fmaxf(m, part_m[i][h]);
-    const bool any = part_m[k][h] > -INFINITY;
-    f_m[k][h] = any ? exp2_fast(part_m[k][h] - m) : 0.f;
-    f_j[k][h] = any ? exp2_fast(part_j[k][h] + 10.f - m) : 0.f;
+      for (int g = 0; g < QG; ++g) load_new(qp + 32 * g, q[g]);
+#pragma unroll
+      for (int g = 0; g < QG; ++g) {
+        gs[g] = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          most = fmaxf(most, fabsf(q[g][e]));
+          gs[g] += q[g][e];
+        }
+        gs[g] += __shfl_xor_sync(0xffffffffu, gs[g], 1);
+        gs[g] += __shfl_xor_sync(0xffffffffu, gs[g], 2);
+        gs[g] *= scale_log2;
+      }
+#pragma unroll
+      for (int o = 1; o < (GT == 1 ? 32 : 4); o <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+      // power of two that brings the largest to [2^13, 2^14)
+      const int ex = min(max(13 + 127 - (int)(__float_as_uint(most) >> 23), -100), 126);
+      const float up = __uint_as_float((uint32_t)(ex + 127) << 23), back = __uint_as_float((uint32_t)(24 - ex + 127) << 23) * scale_log2;
+      uint32_t hi[QG][4], lo[QG][4];
+#pragma unroll
+      for (int g = 0; g < QG; ++g)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const float f = x & 1 ? up * 0.0625f : up, p0 = q[g][x] * f, p1 = q[g][x + 4] * f;      // (odd channels' codes stand four bits higher)
+          const __half2 h = __floats2half2_rn(p0, p1);
+          hi[g][x] = *reinterpret_cast<const uint32_t*>(&h);
+          lo[g][x] = SPLIT_Q ? half2_of(p0 - __low2float(h), p1 - __high2float(h)) : 0u;
+        }
+      if constexpr (GT == 1) {
+#pragma unroll
+        for (int g = 0; g < NG; ++g)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) qb[g][x] = (r8 >> 1) == g ? (r8 & 1 ? lo[0][x] : hi[0][x]) : 0u;
+        q_back[0] = back;
+        qsum[0][0] = __shfl_sync(0xffffffffu, gs[0], 8 * t4);      // (row 2 t4: group t4)
+        qsum[0][1] = 0.f;
+        if (t4 >= NG) qsum[0][0] = 0.f;
+      } else {
+#pragma unroll
+        for (int g = 0; g < NG; ++g)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            qb[g][x] = hi[g][x];
+            if constexpr (SPLIT_Q) qr[g][x] = lo[g][x];
+          }
+        // (an accumulator's columns are heads 2 t4 and 2 t4 + 1; their sums are with the lanes of those columns)
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          q_back[x] = __shfl_sync(0xffffffffu, back, 4 * (2 * t4 + x));
+#pragma unroll
+          for (int g = 0; g < NG; ++g) qsum[g][x] = __shfl_sync(0xffffffffu, gs[g], 4 * (2 * t4 + x));
+        }
+      }
+    }
+
+    // ---- the ring: the next item, its slot and the parity of its barrier; the next item to request
+    int n = tiles_in(cnt), slot = 0, next = early;
+    uint32_t par = 0;
+    auto arrived = [&]() {
+      if (!bad && !bar_wait(&full[wid][slot], par)) bad = true;
+    };
+    auto release = [&]() {                    // every lane has read the item: its slot takes the next one
+      __syncwarp();
+      if (next < 2 * n) {
+        if (lane == 0 && !bad) request(next, n, slot);
+        ++next;
+      }
+      if (++slot == depth) { slot = 0; par ^= 1; }
+    };
+    bool fresh = true;                        // the early items were requested before the launch ahead had completed
+    if (n != n_alloc) {                       // fewer tokens than there is room for: what was requested early is dropped
+      const int dropped = early;
+      next = 2 * n;
+      for (int j = 0; j < dropped; ++j) { arrived(); release(); }
+      next = min(depth, 2 * n);
+      if (lane == 0 && !bad)
+        for (int j = 0; j < next; ++j) request(j, n, (slot + j) % depth);
+      __syncwarp();
+      fresh = false;
+    }
+    // the row that the launch ahead appended, for the early item that holds it (lanes below CODES / 4: codes, then parameters)
+    const int ls_item = fresh && ls >= 0 && ls != fs && ls_local >= 0 && ls_local < cnt && ls_local / Q4_TILE % Q4_WARPS == wid
+                            ? ls_local / (Q4_TILE * Q4_WARPS) : -1;
+    uint32_t ls_word[2] = {0u, 0u};
+    if (ls_item >= 0) {
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        if (lane < CODES / 4) ls_word[x] = load_fresh(reinterpret_cast<const uint32_t*>((x ? vc : kc) + (int64_t)ls_local * CODES) + lane);
+        else if (lane < CODES / 4 + NG) ls_word[x] = load_fresh(reinterpret_cast<const uint32_t*>((x ? vp : kp) + (int64_t)ls_local * PARAMS) + (lane - CODES / 4));
+      }
+    }
+    auto patch = [&](int j, int x) {          // item j (of K: x = 0, of V: x = 1)
+      if (j == ls_item && (x ? n : 0) + j < early) {
+        unsigned char* row = ring + slot * ITEM;
+        const int r = ls_local % Q4_TILE;
+        if (lane < CODES / 4) reinterpret_cast<uint32_t*>(row + r * CODES)[lane] = ls_word[x];
+        else if (lane < CODES / 4 + NG) reinterpret_cast<uint32_t*>(row + Q4_TILE * CODES + r * PARAMS)[lane - CODES / 4] = ls_word[x];
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // (before the next bulk copy into the slot)
+        __syncwarp();
+      }
+    };
+
+    // ---- logits of this warp's tiles and their maximum
+    constexpr int MX = GT > 1 ? 2 : 1;
+    float m_run[MX];
+#pragma unroll
+    for (int x = 0; x < MX; ++x) m_run[x] = -INFINITY;
+    auto k_tiles = [&](int j0, auto tiles) {
+      constexpr int N = decltype(tiles)::value;
+      uint32_t kw[N][2][KW], pr[N][2][KP];
+#pragma unroll
+      for (int a = 0; a < N; ++a) {
+        arrived();
+        patch(j0 + a, 0);
+        const unsigned char* tile = ring + slot * ITEM;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          words_of(tile + (r8 + 8 * i) * CODES + t4 * (HD / 8), kw[a][i]);
+          if constexpr (GT == 1) pr[a][i][0] = t4 < NG ? *reinterpret_cast<const uint32_t*>(tile + Q4_TILE * CODES + (r8 + 8 * i) * PARAMS + 4 * t4) : 0u;
+          else words_of(tile + Q4_TILE * CODES + (r8 + 8 * i) * PARAMS, pr[a][i]);
+        }
+        release();
+      }
+      float acc[N][GT > 1 ? NG : 2][4];
+#pragma unroll
+      for (int a = 0; a < N; ++a)
+#pragma unroll
+        for (int g = 0; g < (GT > 1 ? NG : 2); ++g) acc[a][g][0] = acc[a][g][1] = acc[a][g][2] = acc[a][g][3] = 0.f;
+#pragma unroll
+      for (int g = 0; g < NG; ++g)
+#pragma unroll
+        for (int a = 0; a < N; ++a) {
+          // words of chunks 2 t4 (first half of the lane's words) and 2 t4 + 1; a half word is a group
+          const uint32_t sel = g & 1 ? 0x7632u : 0x5410u;
+          const uint32_t xa = __byte_perm(kw[a][0][g >> 1], kw[a][0][KW / 2 + (g >> 1)], sel), xb = __byte_perm(kw[a][1][g >> 1], kw[a][1][KW / 2 + (g >> 1)], sel);
+          const uint32_t ya = xa >> 8, yb = xb >> 8;
+          float(&d0)[4] = acc[a][GT > 1 ? g : 0];
+          float(&d1)[4] = acc[a][GT > 1 ? g : 1];
+          mma_f16(d0, xa & 0x000f000fu, xb & 0x000f000fu, xa & 0x00f000f0u, xb & 0x00f000f0u, qb[g][0], qb[g][1]);
+          mma_f16(d1, ya & 0x000f000fu, yb & 0x000f000fu, ya & 0x00f000f0u, yb & 0x00f000f0u, qb[g][2], qb[g][3]);
+          if constexpr (GT > 1 && SPLIT_Q) {
+            mma_f16(d0, xa & 0x000f000fu, xb & 0x000f000fu, xa & 0x00f000f0u, xb & 0x00f000f0u, qr[g][0], qr[g][1]);
+            mma_f16(d1, ya & 0x000f000fu, yb & 0x000f000fu, ya & 0x00f000f0u, yb & 0x00f000f0u, qr[g][2], qr[g][3]);
+          }
+        }
+#pragma unroll
+      for (int a = 0; a < N; ++a)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int row = tile_row(j0 + a) + r8 + 8 * i;
+          const bool live = row < cnt && row != fs_local;      // (the incoming token's slot is the ninth warp's)
+          float s[MX];
+          if constexpr (GT == 1) {
+            const float d = (acc[a][0][2 * i] + acc[a][1][2 * i]) + (acc[a][0][2 * i + 1] + acc[a][1][2 * i + 1]);
+            s[0] = fmaf(q4_scale(pr[a][i][0]) * q_back[0], d, q4_low(pr[a][i][0]) * qsum[0][0]);
+            s[0] += __shfl_xor_sync(0xffffffffu, s[0], 1);
+            s[0] += __shfl_xor_sync(0xffffffffu, s[0], 2);
+          } else {
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+              float d = 0.f, l = 0.f;
+#pragma unroll
+              for (int g = 0; g < NG; ++g) {
+                d = fmaf(q4_scale(pr[a][i][g]), acc[a][g][2 * i + x], d);
+                l = fmaf(q4_low(pr[a][i][g]), qsum[g][x], l);
+              }
+              s[x] = fmaf(d, q_back[x], l);
+            }
+          }
+#pragma unroll
+          for (int x = 0; x < MX; ++x) {
+            if (!live) s[x] = -INFINITY;
+            const int h = GT > 1 ? 2 * t4 + x : 0;
+            if ((GT > 1 ? h < G : t4 == 0) && row != fs_local) logit_s[h * chunk + row] = s[x];
+            m_run[x] = fmaxf(m_run[x], s[x]);
+          }
+        }
+    };
+    {
+      int j = 0;
+      for (; j + NT <= n; j += NT) k_tiles(j, std::integral_constant<int, NT>{});
+      if (j < n) k_tiles(j, std::integral_constant<int, 1>{});
+    }
+    // (after the wait: at most one unfinished predecessor exists while a successor sets up)
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+#pragma unroll
+    for (int x = 0; x < MX; ++x) {
+#pragma unroll
+      for (int o = 4; o < 32; o <<= 1) m_run[x] = fmaxf(m_run[x], __shfl_xor_sync(0xffffffffu, m_run[x], o));
+      const int h = GT > 1 ? 2 * t4 + x : 0;
+      if (r8 == 0 && (GT > 1 ? h < G : t4 == 0)) part_m[wid][h] = m_run[x];
+    }
+    __syncwarp();
+    if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(s32(&k_done)) : "memory");
+
+    // ---- O^T += V^T (p sc): A = codes (16 channels x 16 slots), B = p sc by slot and head, scaled by 2^(13 - J) to fit fp16.  J follows
+    // the largest s + log2 sc (rounded up) with a slack of 2^2; when it moves, the accumulators are rescaled (a power of two).
+    float o_acc[NG][2][4];
+#pragma unroll
+    for (int g = 0; g < NG; ++g)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) o_acc[g][i][0] = o_acc[g][i][1] = o_acc[g][i][2] = o_acc[g][i][3] = 0.f;
+    float m_own[GT], l_run[GT], lo_run[GT][VW];      // this warp's maxima; of this lane's slots (and groups): sum of p, sum of p lo
+    int J[GT];
+#pragma unroll
+    for (int h = 0; h < GT; ++h) {
+      m_own[h] = GT == 1 || h < G ? part_m[wid][h] : -INFINITY;
+      l_run[h] = 0.f;
+      J[h] = -100000000;
+#pragma unroll
+      for (int i = 0; i < VW; ++i) lo_run[h][i] = 0.f;
+    }
+    auto v_tiles = [&](int j0, auto tiles) {
+      constexpr int N = decltype(tiles)::value;
+      bool live[N];
+      float s[N][GT];
+      uint32_t vw[N][4][VW], pr[N][VW];
+#pragma unroll
+      for (int a = 0; a < N; ++a) {
+        const int row = tile_row(j0 + a) + (lane >> 1);
+        live[a] = row < cnt && row != fs_local;
+#pragma unroll
+        for (int h = 0; h < GT; ++h) s[a][h] = (GT == 1 || h < G) && live[a] ? logit_s[h * chunk + row] : -INFINITY;
+        arrived();
+        patch(j0 + a, 1);
+        const unsigned char* tile = ring + slot * ITEM;
+        words_of(tile + Q4_TILE * CODES + (lane >> 1) * PARAMS + (lane & 1) * VW * 4, pr[a]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) words_of(tile + (4 * i + t4) * CODES + r8 * (HD / 16), vw[a][i]);
+        release();
+      }
+      int ev[N];                             // exponent of the largest scale, rounded up (2^-100 is the least, 0 apart)
+#pragma unroll
+      for (int a = 0; a < N; ++a) {
+        ev[a] = -100;
+#pragma unroll
+        for (int i = 0; i < VW; ++i) {
+          if (!live[a]) pr[a][i] = 0u;
+          ev[a] = max(ev[a], (int)(pr[a][i] >> 7 & 0xffu) - 126);
+        }
+      }
+      bool moved = false;
+      float f[GT];
+#pragma unroll
+      for (int h = 0; h < GT; ++h) {
+        f[h] = 1.f;
+        if (GT == 1 || h < G) {
+          int top = -100000000;
+#pragma unroll
+          for (int a = 0; a < N; ++a) top = live[a] ? max(top, (int)ceilf(fminf(fmaxf(s[a][h], -4e6f), 4e6f)) + ev[a]) : top;
+          top = __reduce_max_sync(0xffffffffu, top);
+          if (top > J[h] + 2) {
+            f[h] = exp2_fast((float)(J[h] - top));
+            J[h] = top;
+            moved = true;
+          }
+        }
+      }
+      if (moved) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          float fx = f[0];                   // of column 2 t4 + x
+#pragma unroll
+          for (int h = 1; h < GT; ++h) fx = (GT > 4 ? 2 * t4 + x : t4) == h ? f[h] : fx;
+#pragma unroll
+          for (int g = 0; g < NG; ++g)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) { o_acc[g][i][x] *= fx; o_acc[g][i][2 + x] *= fx; }
+        }
+      }
+#pragma unroll
+      for (int a = 0; a < N; ++a)
+#pragma unroll
+        for (int h = 0; h < GT; ++h)
+          if (GT == 1 || h < G) {
+            const float p = live[a] ? exp2_fast(s[a][h] - m_own[h]) : 0.f, y = live[a] ? exp2_fast(s[a][h] - (float)(J[h] - 13)) : 0.f;
+            l_run[h] += p;
+#pragma unroll
+            for (int i = 0; i < VW; ++i) {
+              const float x = y * q4_scale(pr[a][i]);
+              lo_run[h][i] = fmaf(p, q4_low(pr[a][i]), lo_run[h][i]);
+              const __half hh = __float2half_rn(x), hl = __float2half_rn(x - __half2float(hh));
+              uint16_t* to = &xs[wid][a][(lane & 1) * VW + i][x_col(h, 0)][4 * (lane >> 1 & 3) + (lane >> 3)];
+              to[0] = __half_as_ushort(hh);
+              to[(x_col(h, 1) - x_col(h, 0)) * Q4_TILE] = __half_as_ushort(hl);
+            }
+          }
+      __syncwarp();
+#pragma unroll
+      for (int a = 0; a < N; ++a)
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+          const uint2 b = *reinterpret_cast<const uint2*>(&xs[wid][a][g][r8][4 * t4]);
+          const uint32_t sel = g & 1 ? 0x7632u : 0x5410u;
+          const uint32_t xa = __byte_perm(vw[a][0][g >> 1], vw[a][1][g >> 1], sel), xb = __byte_perm(vw[a][2][g >> 1], vw[a][3][g >> 1], sel);
+          const uint32_t ya = xa >> 8, yb = xb >> 8;
+          mma_f16(o_acc[g][0], xa & 0x000f000fu, xa & 0x00f000f0u, xb & 0x000f000fu, xb & 0x00f000f0u, b.x, b.y);
+          mma_f16(o_acc[g][1], ya & 0x000f000fu, ya & 0x00f000f0u, yb & 0x000f000fu, yb & 0x00f000f0u, b.x, b.y);
+          if constexpr (GT > 4) {
+            const uint2 d = *reinterpret_cast<const uint2*>(&xs[wid][a][g][8 + r8][4 * t4]);
+            mma_f16(o_acc[g][0], xa & 0x000f000fu, xa & 0x00f000f0u, xb & 0x000f000fu, xb & 0x00f000f0u, d.x, d.y);
+            mma_f16(o_acc[g][1], ya & 0x000f000fu, ya & 0x00f000f0u, yb & 0x000f000fu, yb & 0x00f000f0u, d.x, d.y);
+          }
+        }
+      __syncwarp();
+    };
+    {
+      int j = 0;
+      for (; j + NT <= n; j += NT) v_tiles(j, std::integral_constant<int, NT>{});
+      if (j < n) v_tiles(j, std::integral_constant<int, 1>{});
+    }
+    fetch(tid);
+    // ---- the warp's partial, relative to the CTA's maximum: sums of p (even lanes) and of p lo, and O^T with its constant factors
+    // (codes in odd channels stand four bits higher), into the ring
+    if (!bad && !bar_wait(&k_done, 0)) bad = true;
+    __syncwarp();
+    float fo[2] = {0.f, 0.f};                // of this lane's columns
+#pragma unroll
+    for (int h = 0; h < GT; ++h)
+      if (GT == 1 || h < G) {
+        float m = m_own[h];
+#pragma unroll
+        for (int k = 0; k <= Q4_WARPS; ++k) m = fmaxf(m, part_m[k][h]);
+        const bool any = m_own[h] > -INFINITY;
+        const float fm = any ? exp2_fast(m_own[h] - m) : 0.f, fj = any ? exp2_fast((float)(J[h] + 11) - m) : 0.f;
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+          if ((GT > 4 ? 2 * t4 + x : t4) == h) fo[x] = fj;
+#pragma unroll
+        for (int o = 2; o < 32; o <<= 1) {
+          l_run[h] += __shfl_xor_sync(0xffffffffu, l_run[h], o);
+#pragma unroll
+          for (int i = 0; i < VW; ++i) lo_run[h][i] += __shfl_xor_sync(0xffffffffu, lo_run[h][i], o);
+        }
+        if (lane < 2) {
+          if (lane == 0) part_l[wid][h] = l_run[h] * fm;
+#pragma unroll
+          for (int i = 0; i < VW; ++i) part_lo[wid][h][lane * VW + i] = lo_run[h][i] * fm;
+        }
+      }
+    float* po = reinterpret_cast<float*>(ring);
+#pragma unroll
+    for (int x = 0; x < (GT > 4 ? 2 : 1); ++x) {
+      const int h = GT > 4 ? 2 * t4 + x : t4;
+      if (h < G) {
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+          float o[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i)        // channel 4 r8 + i of the group; the remainder's column beside it
+            o[i] = (GT > 4 ? o_acc[g][i >> 1][2 * (i & 1) + x] : o_acc[g][i >> 1][2 * (i & 1)] + o_acc[g][i >> 1][2 * (i & 1) + 1]) * (i & 1 ? fo[x] * 0.0625f : fo[x]);
+          *reinterpret_cast<float4*>(po + h * HD + 32 * g + 4 * r8) = make_float4(o[0], o[1], o[2], o[3]);
+        }
+      }
+    }
   }
   __syncthreads();
-  // (another CTA's shared memory may only be written once that CTA runs and its barriers are armed)
   if (split > 1) cluster_wait_acquire();
 
   // ---- to the unit's CTAs: maximum and sum to every one, channel slice r of the partial output to rank r
   const int slice = HD / split, slice_log2 = 31 - __clz(slice);
   if (tid < split * G) {
     const int h = tid / split, dst = tid - h * split;
-    float m = part_m[0][h], l = 0.f;
+    float m = part_m[Q4_WARPS][h], l = part_l[Q4_WARPS][h];
 #pragma unroll
     for (int k = 0; k < Q4_WARPS; ++k) {
       m = fmaxf(m, part_m[k][h]);
-      l = fmaf(part_l[k][h], f_m[k][h], l);
+      l += part_l[k][h];
     }
-    if (split > 1) send2(at_rank(s32(&ex_ml[rank][h]), dst), m, l, at_rank(s32(&ex_bar), dst));
-    else ex_ml[0][h] = make_float2(m, l);
+    send2(at_rank(s32(&ex_ml[rank][h]), dst), m, l, at_rank(s32(&ex_bar), dst));
   }
   for (int i = tid; i < G * HD; i += Q4_THREADS) {
     const int h = i / HD, ch = i - h * HD;
-    float a = 0.f;
+    float a = new_o[i];
 #pragma unroll
-    for (int k = 0; k < Q4_WARPS; ++k) {
-      a = fmaf(part_o[((size_t)k * G + h) * HD + ch], f_j[k][h], a);
-      a = fmaf(part_lo[k][h][ch >> 5], f_m[k][h], a);
-    }
-    const int dst = ch >> slice_log2, off = (rank * G + h) * slice + (ch & (slice - 1));
-    if (split > 1) send(at_rank(s32(&xo[off]), dst), a, at_rank(s32(&ex_bar), dst));
-    else xo[off] = a;
+    for (int k = 0; k < Q4_WARPS; ++k) a += reinterpret_cast<const float*>(dyn + (size_t)k * ring_bytes)[i] + part_lo[k][h][ch >> 5];
+    const int dst = ch >> slice_log2;
+    send(at_rank(s32(&xo[(rank * G + h) * slice + (ch & (slice - 1))]), dst), a, at_rank(s32(&ex_bar), dst));
   }
-  bool bad = false;                      // this thread's wait ran out: the results are void
-  if (split > 1) bad = !bar_wait(&ex_bar);
-  else __syncthreads();
+  if (!bar_wait(&ex_bar, 0)) bad = true;
 
   // ---- every CTA: the unit's normaliser (all data is local now) and its slice of the output
   float m_all = -INFINITY, inv_all = 0.f;      // of the one head
@@ -653,110 +792,119 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int B, int cap, int F,
     }
   }
 
-  // ---- indicator update (Eq. 2 / Eq. 3) and importance (Eq. 4) of this CTA's slots, its arg-min
+  // ---- indicator update (Eq. 2 / Eq. 3) and importance (Eq. 4) of this CTA's slots, every warp's arg-min to rank 0
   const bool evicting = hi > B;
-  unsigned long long my_key = Q4_NO_KEY;
-  int my_slot = -1, my_pos = -1;
-  for (int i0 = tid; i0 < cnt;) {
+  if (wid < Q4_WARPS) {
+    unsigned long long my_key = Q4_NO_KEY;
+    int my_slot = -1, my_pos = -1;
+    for (int i0 = tid; i0 < cnt;) {
 #pragma unroll
-    for (int k = 0; k < SB; ++k) {
-      const int i = i0 + k * Q4_THREADS;
-      if (i >= cnt) continue;
-      float p;
-      if constexpr (GT == 1) {
-        p = exp2_fast(logit_s[i] - m_all) * inv_all;
-      } else {                             // the mean of the heads' probabilities
-        p = 0.f;
+      for (int k = 0; k < SB; ++k) {
+        const int i = i0 + k * Q4_WORKERS;
+        if (i >= cnt) continue;
+        float p;
+        if constexpr (GT == 1) {
+          p = exp2_fast(logit_s[i] - m_all) * inv_all;
+        } else {                             // the mean of the heads' probabilities
+          p = 0.f;
 #pragma unroll
-        for (int h = 0; h < GT; ++h)
-          if (h < G) p = fmaf(exp2_fast(logit_s[h * ld + i] - all_m[h]), all_inv[h], p);
-        p /= (float)G;
+          for (int h = 0; h < GT; ++h)
+            if (h < G) p = fmaf(exp2_fast(logit_s[h * chunk + i] - all_m[h]), all_inv[h], p);
+          p /= (float)G;
+        }
+        const bool is_new = i == fs_local;
+        const int64_t o = base + i;
+        float S;
+        if (WINDOWED) {
+          const long long fx = is_new ? prob_to_fixed(p) : fx_r[k] + prob_to_fixed(p) - prob_to_fixed(old_r[k]);
+          c.state.ring[((int64_t)u * w + (t % w)) * cap + s0 + i] = p;
+          c.state.acc_fixed[o] = fx;
+          S = fixed_to_prob(fx);
+        } else {
+          S = is_new ? p : old_r[k] + p;
+        }
+        if (VATP_INB(s0 + i, cap, dev_status)) c.state.acc[o] = S;
+        const int ps = is_new ? t : pos_r[k];
+        if (evicting && ps >= F && ps <= t - R) {
+          const unsigned long long key = q4_evict_key(S * (is_new ? new_norm_s : norm_r[k]), ps);
+          if (key < my_key) { my_key = key; my_slot = s0 + i; my_pos = ps; }
+        }
       }
-      const bool is_new = i == fs_local;
-      const int64_t o = base + i;
-      float S;
-      if (WINDOWED) {
-        const long long fx = is_new ? prob_to_fixed(p) : fx_r[k] + prob_to_fixed(p) - prob_to_fixed(old_r[k]);
-        c.state.ring[((int64_t)u * w + (t % w)) * cap + s0 + i] = p;
-        c.state.acc_fixed[o] = fx;
-        S = fixed_to_prob(fx);
-      } else {
-        S = is_new ? p : old_r[k] + p;
-      }
-      c.state.acc[o] = S;
-      const int ps = is_new ? t : pos_r[k];
-      if (evicting && ps >= F && ps <= t - R) {
-        const unsigned long long key = q4_evict_key(S * (is_new ? new_norm_s : norm_r[k]), ps);
-        if (key < my_key) { my_key = key; my_slot = s0 + i; my_pos = ps; }
-      }
+      i0 += SB * Q4_WORKERS;
+      if (i0 < cnt) fetch(i0);
     }
-    i0 += SB * Q4_THREADS;
-    if (i0 < cnt) fetch(i0);
-  }
-  if (WINDOWED) {
-    // recycled slot: the other rows of its ring column belong to the previous occupant (shared out over the unit's CTAs)
-    for (int r = rank * Q4_THREADS + tid; r < w; r += split * Q4_THREADS)
-      if (r != t % w) c.state.ring[((int64_t)u * w + r) * cap + fs] = 0.f;
-  }
-  if (evicting) {
-    // this CTA's candidate (positions are unique: one thread holds the winning key), sent to rank 0
-    const unsigned long long wkey = min_key(my_key);
-    if (lane == 0) warp_key[wid] = wkey;
-    __syncthreads();
-    const unsigned long long win = min_key(lane < Q4_WARPS ? warp_key[lane] : Q4_NO_KEY);
-    if (win == Q4_NO_KEY ? tid == 0 : my_key == win) {
-      if (split > 1)
-        send4(at_rank(s32(&cand[rank]), 0), (uint32_t)win, (uint32_t)(win >> 32), (uint32_t)my_slot, (uint32_t)my_pos, at_rank(s32(&cand_bar), 0));
-      else
-        cand[0] = Q4Candidate{win, my_slot, my_pos};
+    if (WINDOWED) {
+      // recycled slot: the other rows of its ring column belong to the previous occupant (shared out over the unit's CTAs)
+      for (int r = rank * Q4_WORKERS + tid; r < w; r += split * Q4_WORKERS)
+        if (r != t % w) c.state.ring[((int64_t)u * w + r) * cap + fs] = 0.f;
     }
-    if (split == 1) __syncthreads();
-  }
-  if (rank == 0 && tid == 0) {
-    int out_slot = hi, left = hi, ev = -1;                         // not evicting: the cache grows
     if (evicting) {
-      if (split > 1 && !bar_wait(&cand_bar)) bad = true;
+      // (positions are unique: one lane holds the winning key)
+      const unsigned long long win = min_key(my_key);
+      if (win == Q4_NO_KEY ? lane == 0 : my_key == win)
+        send4(at_rank(s32(&cand[rank * Q4_WARPS + wid]), 0), (uint32_t)win, (uint32_t)(win >> 32), (uint32_t)my_slot, (uint32_t)my_pos, at_rank(s32(&cand_bar), 0));
+    }
+  } else if (rank == 0) {
+    int out_slot = hi, left = hi, ev = -1;                         // not evicting: the cache grows
+    bool write = lane == 0;
+    if (evicting) {
+      if (!bar_wait(&cand_bar, 0)) bad = true;
       Q4Candidate best{Q4_NO_KEY, -1, -1};
-      for (int r = 0; r < split; ++r)
-        if (cand[r].key < best.key) best = cand[r];
-      if (best.key != Q4_NO_KEY) {
+      for (int i = lane; i < split * Q4_WARPS; i += 32)
+        if (cand[i].key < best.key) best = cand[i];
+      const unsigned long long win = min_key(best.key);
+      if (win != Q4_NO_KEY) {
+        write = best.key == win;
         out_slot = best.slot;
         ev = best.pos;
         left = hi - 1;
-        c.state.pos[(int64_t)u * cap + out_slot] = -1;
+        if (write && VATP_INB(out_slot, cap, dev_status)) c.state.pos[(int64_t)u * cap + out_slot] = -1;
       } else {                             // nothing eligible (cannot happen when F + R <= B): keep the state consistent
         out_slot = min(hi, cap - 1);
       }
     }
-    c.state.len[u] = left;
-    c.state.free_slot[u] = out_slot;
-    c.state.next_pos[u] = t + 1;
-    c.state.last_slot[u] = fs;
-    if (evicted) evicted[u] = ev;
+    if (write) {
+      c.state.len[u] = left;
+      c.state.free_slot[u] = out_slot;
+      c.state.next_pos[u] = t + 1;
+      c.state.last_slot[u] = fs;
+      if (evicted) evicted[u] = ev;
+    }
   }
   if (bad) {
-    // Something never arrived: say so, and stay until the unit's other CTAs have sent what they send here (threads that exit count
-    // as arrived).
+    // Something never arrived: say so, give copies that may still be in flight time to land, and stay until the unit's other CTAs have
+    // sent what they send here (threads that exit count as arrived).
     if (dev_status) atomicExch(dev_status, (int)VATP_ERR_TIMEOUT);
     for (int i = 0; i < 200; ++i) __nanosleep(1000);
   }
 }
 
+#ifndef Q4_FILL
+#define Q4_FILL 1
+#endif
 template <typename T, int HD, int GT>
 cudaError_t launch_gt(int units, int G, int B, int F, int R, int window, int norm, float scale, const vatp_cache_q4& c, const void* q,
                       const void* k, const void* v, void* out, int32_t* evicted, int32_t* dev_status, cudaStream_t st) {
   const int cap = cache_capacity(B), sms = device_sm_count();
-  // The logits of a CTA's slots stand in shared memory beside the warps' partial outputs.
-  const size_t most = 200 * 1024, partials = (size_t)Q4_WARPS * G * HD * 4;
+  constexpr int ITEM = q4_item<HD>;
+  // Static arrays and what the system takes, rounded up; half of an SM's shared memory and all of it.
+  constexpr size_t fixed = (GT > 4 ? 27 : GT > 1 ? 23 : 21) * 1024, half_sm = 113 * 1024 - fixed, whole_sm = 226 * 1024 - fixed;
   auto chunk_of = [&](int split) { return ((cap + split - 1) / split + Q4_TILE - 1) / Q4_TILE * Q4_TILE; };
+  // a ring takes the warp's partial output in the end
+  const int least = (G * HD * 4 + ITEM - 1) / ITEM > 2 ? (G * HD * 4 + ITEM - 1) / ITEM : 2;
+  auto bytes = [&](int split, int depth) { return (size_t)Q4_WARPS * depth * ITEM + (size_t)G * HD * 4 + (size_t)G * chunk_of(split) * 4; };
   int split = 1;
-  while (split < Q4_SPLIT && units * split * 2 <= 2 * sms && cap / (split * 2) >= 4 * Q4_TILE) split *= 2;
-  while (split < Q4_SPLIT && partials + (size_t)G * chunk_of(split) * 4 > most) split *= 2;
-  const int chunk = chunk_of(split);
-  const size_t dyn = partials + (size_t)G * chunk * 4;
-  if (dyn > most || (int64_t)units * split > 0x7fffffffll) return cudaErrorNotSupported;
+  while (split < Q4_SPLIT && units * split * 2 <= Q4_FILL * sms && cap / (split * 2) >= 4 * Q4_TILE) split *= 2;
+  while (split < Q4_SPLIT && bytes(split, least) > whole_sm) split *= 2;
+  const int chunk = chunk_of(split), per_warp = (chunk / Q4_TILE + Q4_WARPS - 1) / Q4_WARPS;
+  int depth = 2 * per_warp;
+  depth = depth < least ? least : depth > Q4_DEPTH ? Q4_DEPTH : depth;
+  const size_t limit = bytes(split, least) <= half_sm ? half_sm : whole_sm;
+  while (depth > least && bytes(split, depth) > limit) --depth;
+  const size_t dyn = bytes(split, depth);
+  if (dyn > whole_sm || (int64_t)units * split > 0x7fffffffll) return cudaErrorNotSupported;
   auto kern = window > 0 ? decode_q4_kernel<T, HD, true, GT> : decode_q4_kernel<T, HD, false, GT>;
-  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most);
+  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)whole_sm);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(units * split));
@@ -772,7 +920,7 @@ cudaError_t launch_gt(int units, int G, int B, int F, int R, int window, int nor
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, kern, G, split, chunk, chunk, B, cap, F, R, window, norm, scale * Q4_LOG2E, c, (const T*)q, (const T*)k,
+  return cudaLaunchKernelEx(&cfg, kern, G, split, chunk, depth, B, cap, F, R, window, norm, scale * Q4_LOG2E, c, (const T*)q, (const T*)k,
                             (const T*)v, (T*)out, evicted, dev_status);
 }
 
