@@ -22,8 +22,6 @@
 #include <cooperative_groups.h>
 #include <cuda_fp16.h>
 
-#include <type_traits>
-
 #include "q4.cuh"
 
 namespace cg = cooperative_groups;
@@ -33,10 +31,11 @@ namespace {
 
 constexpr int Q4_WARPS = 8;            // that take slots
 constexpr int Q4_WORKERS = Q4_WARPS * 32, Q4_THREADS = Q4_WORKERS + 32;
-constexpr int Q4_TILE = 16;            // slots of a warp at a time
+constexpr int Q4_TILE = 16;            // slots of an MMA tile
+constexpr int Q4_ROWS = 32;            // slots of a warp at a time: an item of its ring
 constexpr int Q4_SPLIT = 8;            // CTAs of a unit at most
 constexpr int Q4_HEADS = 8;            // query heads of a unit at most (columns of the MMA tiles)
-constexpr int Q4_DEPTH = 16;           // tiles in a warp's ring at most
+constexpr int Q4_DEPTH = 8;            // items in a warp's ring at most
 constexpr float Q4_LOG2E = 1.4426950408889634f;
 constexpr unsigned long long Q4_NO_KEY = ~0ull;
 
@@ -44,20 +43,21 @@ __device__ __forceinline__ uint32_t s32(const void* p) { return (uint32_t)__cvta
 __device__ __forceinline__ void bar_init(uint64_t* bar, uint32_t count) {
   asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(s32(bar)), "r"(count) : "memory");
 }
-__device__ __forceinline__ void bar_expect(uint64_t* bar, uint32_t bytes) {
-  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(s32(bar)), "r"(bytes) : "memory");
+__device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
-__device__ __forceinline__ bool bar_try(uint64_t* bar, uint32_t parity) {
+__device__ __forceinline__ void bar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+__device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
   uint32_t ok;
   asm volatile(
       "{\n\t.reg .pred p;\n\t"
       "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
       "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok) : "r"(s32(bar)), "r"(parity) : "memory");
+      : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
   return ok != 0;
 }
 // bounded wait (about a second): false when what the barrier counts never arrived
-__device__ __forceinline__ bool bar_wait(uint64_t* bar, uint32_t parity) {
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity) {
   if (bar_try(bar, parity)) return true;
   uint64_t t0, t1;
   asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t0));
@@ -68,9 +68,9 @@ __device__ __forceinline__ bool bar_wait(uint64_t* bar, uint32_t parity) {
   return true;
 }
 // global -> shared bulk copy; dst, src and bytes are multiples of 16
-__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint64_t* bar) {
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-               ::"r"(dst), "l"(src), "r"(bytes), "r"(s32(bar)) : "memory");
+               ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
 // address of `addr` (this CTA's shared memory) in CTA `rank` of the cluster
 __device__ __forceinline__ uint32_t at_rank(uint32_t addr, int rank) {
@@ -94,6 +94,19 @@ __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1,
   asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// D (16x8, int32) = A (16x32, u8, row) * B (32x8, s8 or u8, col) + C
+__device__ __forceinline__ void mma_s8(int (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1, int c) {
+  asm("mma.sync.aligned.m16n8k32.row.col.s32.u8.s8.s32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+      : "=r"(d[0]), "=r"(d[1]), "=r"(d[2]), "=r"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "r"(c));
+}
+__device__ __forceinline__ void mma_s8(int (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k32.row.col.s32.u8.s8.s32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+r"(d[0]), "+r"(d[1]), "+r"(d[2]), "+r"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_u8(int (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k32.row.col.s32.u8.u8.s32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+r"(d[0]), "+r"(d[1]), "+r"(d[2]), "+r"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ float exp2_fast(float x) {
   float y;
@@ -166,18 +179,21 @@ __device__ __forceinline__ unsigned long long min_key(unsigned long long key) {
 // remainders; 8 - five to eight, a column a head and two products.
 // Dynamic shared memory: rings [8][depth][tile], which take the warps' partial outputs in the end | the ninth partial [G][HD] |
 // logits [G][chunk].
-template <int HD> constexpr int q4_item = Q4_TILE * (HD / 2 + HD / 8);      // bytes of a tile: codes, then parameters
+template <int HD> constexpr int q4_item = Q4_ROWS * (HD / 2 + HD / 8);      // bytes of an item: codes, then parameters
 
 template <typename T, int HD, bool WINDOWED, int GT>
 __global__ void __launch_bounds__(Q4_THREADS, 2)
 decode_q4_kernel(int G_arg, int split, int chunk, int depth, int B, int cap, int F, int R, int w, int norm, float scale_log2, vatp_cache_q4 c, const T* q_new,
                  const T* k_new, const T* v_new, T* out, int32_t* evicted, int32_t* dev_status) {
   constexpr int NG = HD / 32, KW = HD / 32, VW = HD / 64;       // groups of a row; 32-bit words of a lane in a K row and a V row
-  constexpr int KP = GT == 1 ? 1 : NG;                          // parameter words of a lane per K row
-  constexpr int CODES = HD / 2, PARAMS = NG * 4, ITEM = q4_item<HD>;      // bytes of a row's codes and parameters, of a tile
+  constexpr bool INT = GT == 1;                                 // products in integers (see the top)
+  constexpr int KP = INT ? NG / 2 : NG;                         // parameter words of a lane per K row
+  constexpr int CODES = HD / 2, PARAMS = NG * 4, ITEM = q4_item<HD>;      // bytes of a row's codes and parameters, of an item
   constexpr bool SPLIT_Q = sizeof(T) == 4;                      // q has a remainder beyond its high half
   constexpr int XC = GT > 4 ? 16 : 8;                           // columns of the second product's operand: see x_col
-  constexpr int NT = GT > 4 ? 1 : 2;                            // tiles a warp works on at a time (with eight heads: registers)
+  constexpr int N = GT > 4 ? 1 : 2;                             // tiles a warp works on at a time (with eight heads: registers)
+  constexpr int PG = N == 2 ? NG : VW;                          // groups of a lane where p sc is formed: a slot or half of one
+  constexpr int XS = INT ? NG * 4 * 2 * Q4_TILE : N * NG * XC * Q4_TILE * 2;      // bytes of a warp's second operand
   const int G = GT == 1 ? 1 : G_arg;
   // high half and remainder of head h: neighbours, i.e. in one lane's accumulators, or eight columns apart (two products)
   auto x_col = [](int h, int low) { return GT > 4 ? h + 8 * low : 2 * h + low; };
@@ -185,7 +201,9 @@ decode_q4_kernel(int G_arg, int split, int chunk, int depth, int B, int cap, int
   const int ring_bytes = depth * ITEM;                          // of a warp
   float* new_o = reinterpret_cast<float*>(dyn + Q4_WARPS * ring_bytes);
   float* logit_s = new_o + G * HD;
-  __shared__ __align__(16) uint16_t xs[Q4_WARPS][NT][NG][XC][Q4_TILE];      // [tile][group][column][slot: 4 (slot mod 4) + slot / 4]
+  // the second product's operand, [tile][group][column][slot] of fp16 or [group][digit][tile][slot] of bytes; slot s of a tile
+  // stands at 4 (s mod 4) + s / 4
+  __shared__ __align__(16) unsigned char xs[Q4_WARPS][XS];
   __shared__ float part_m[Q4_WARPS + 1][GT], part_l[Q4_WARPS + 1][GT], part_lo[Q4_WARPS][GT][NG];
   __shared__ float xo[GT * HD];                                         // slices of partial outputs received [split][G][HD / split]
   __shared__ float2 ex_ml[Q4_SPLIT][GT];                                // per rank and head: maximum of its logits, sum of exp2(s - m)
@@ -207,11 +225,11 @@ decode_q4_kernel(int G_arg, int split, int chunk, int depth, int B, int cap, int
   }
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   if (tid == Q4_WORKERS) {
-    bar_expect(&ex_bar, (uint32_t)(8 * G * split + 4 * G * HD));
-    if (rank == 0) bar_expect(&cand_bar, (uint32_t)(split * Q4_WARPS * sizeof(Q4Candidate)));
+    bar_expect(s32(&ex_bar), (uint32_t)(8 * G * split + 4 * G * HD));
+    if (rank == 0) bar_expect(s32(&cand_bar), (uint32_t)(split * Q4_WARPS * sizeof(Q4Candidate)));
   }
   if (wid < Q4_WARPS)      // (columns without a head stay 0)
-    for (int i = lane; i < NT * NG * XC * Q4_TILE / 2; i += 32) reinterpret_cast<uint32_t*>(xs[wid])[i] = 0u;
+    for (int i = lane; i < XS / 4; i += 32) reinterpret_cast<uint32_t*>(xs[wid])[i] = 0u;
   __syncthreads();
   // Another CTA's shared memory may only be written once that CTA runs and its barriers are armed: everyone arrives here and
   // waits (long since satisfied) just before the first remote store.
@@ -223,19 +241,20 @@ decode_q4_kernel(int G_arg, int split, int chunk, int depth, int B, int cap, int
   const unsigned char* kp = static_cast<const unsigned char*>(c.k_params) + base * PARAMS;
   const unsigned char* vp = static_cast<const unsigned char*>(c.v_params) + base * PARAMS;
   unsigned char* ring = dyn + (size_t)wid * ring_bytes;
-  // This warp's tiles: wid, wid + 8, ...; n of them among the first `rows` slots.  Item j < n of its ring is the j-th tile of K,
-  // item n + j of V.
-  auto tiles_in = [&](int rows) { return wid * Q4_TILE < rows ? (rows - wid * Q4_TILE + Q4_WARPS * Q4_TILE - 1) / (Q4_WARPS * Q4_TILE) : 0; };
-  auto tile_row = [&](int j) { return (wid + Q4_WARPS * j) * Q4_TILE; };
+  // This warp's items: rows 32 (wid + 8 j) ..; n of them among the first `rows` slots.  Item j < n of its ring holds rows of K, item
+  // n + j of V.
+  auto items_in = [&](int rows) { return max(rows - wid * Q4_ROWS + Q4_WARPS * Q4_ROWS - 1, 0) / (Q4_WARPS * Q4_ROWS); };
+  auto item_row = [&](int j) { return (wid + Q4_WARPS * j) * Q4_ROWS; };
+  const uint32_t ring_a = s32(ring), full_a = s32(&full[wid < Q4_WARPS ? wid : 0][0]);
   auto request = [&](int j, int n, int slot) {      // one lane: item j into ring slot `slot`
-    const int r0 = tile_row(j < n ? j : j - n), rows = min(Q4_TILE, rows_alloc - r0);      // (8 or 16)
-    uint64_t* bar = &full[wid][slot];
+    const bool is_v = j >= n;
+    const int r0 = item_row(is_v ? j - n : j), rows = min(Q4_ROWS, rows_alloc - r0);      // (a multiple of eight)
+    const uint32_t bar = full_a + 8 * slot, dst = ring_a + slot * ITEM;
     bar_expect(bar, (uint32_t)(rows * (CODES + PARAMS)));
-    const uint32_t dst = s32(ring) + slot * ITEM;
-    bulk_load(dst, (j < n ? kc : vc) + (int64_t)r0 * CODES, rows * CODES, bar);
-    bulk_load(dst + Q4_TILE * CODES, (j < n ? kp : vp) + (int64_t)r0 * PARAMS, rows * PARAMS, bar);
+    bulk_load(dst, (is_v ? vc : kc) + (int64_t)r0 * CODES, rows * CODES, bar);
+    bulk_load(dst + Q4_ROWS * CODES, (is_v ? vp : kp) + (int64_t)r0 * PARAMS, rows * PARAMS, bar);
   };
-  const int n_alloc = wid < Q4_WARPS && rows_alloc > 0 ? tiles_in(rows_alloc) : 0, early = min(depth, 2 * n_alloc);
+  const int n_alloc = wid < Q4_WARPS ? items_in(rows_alloc) : 0, early = min(depth, 2 * n_alloc);
   if (lane == 0)
     for (int j = 0; j < early; ++j) request(j, n_alloc, j);
   __syncwarp();
@@ -309,10 +328,10 @@ decode_q4_kernel(int G_arg, int split, int chunk, int depth, int B, int cap, int
 #pragma unroll
       for (int h = 0; h < GT; ++h)
         if (GT == 1 || h < G) part_m[Q4_WARPS][h] = s[h];
-      asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(s32(&k_done)) : "memory");
+      bar_arrive(s32(&k_done));
     }
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    if (!bar_wait(&k_done, 0)) bad = true;
+    if (!bar_wait(s32(&k_done), 0)) bad = true;
 #pragma unroll
     for (int h = 0; h < GT; ++h) {
       if (GT > 1 && h >= G) continue;
@@ -351,19 +370,18 @@ decode_q4_kernel(int G_arg, int split, int chunk, int depth, int B, int cap, int
   };
 
   if (wid < Q4_WARPS) {
-    // ---- B operand of K q^T.  Lane (n = r8, t4): channels 8 t4 .. 8 t4 + 7 of every group of its column's head.
-    // GT == 1: column 2 g carries the high half of group g alone, column 2 g + 1 its remainder: every lane of a row's four then
-    // holds one group's sum, to be scaled by that group's parameters.  Else: column n is head n.
-    uint32_t qb[NG][4], qr[GT > 1 && SPLIT_Q ? NG : 1][4];
-    float q_back[GT > 1 ? 2 : 1], qsum[GT > 1 ? NG : 1][2];      // 2^24 / (the head's power of two) * scale; sums of q over groups, * scale
+    // ---- B operand of K q^T.  Lane (n = r8, t4): channels 8 t4 .. 8 t4 + 7 of groups of its column.
+    // INT: columns 0 - 3 are the four digits of group 0 (then of group 2), columns 4 - 7 of group 1 (3).  Else: column n is head n.
+    uint32_t qb[NG][INT ? 2 : 4], qr[GT > 1 && SPLIT_Q ? NG : 1][4];
+    // what a sum is to be multiplied by (INT: of the lane's two digits); sums of q over groups, * scale
+    float q_back[2], qsum[INT ? NG / 2 : NG][2];
     {
-      // (GT == 1: of group r8 / 2 alone)
-      constexpr int QG = GT == 1 ? 1 : NG;
-      const int g0 = GT == 1 ? min(r8 >> 1, NG - 1) : 0;
-      const T* qp = q_new + ((int64_t)u * G + (GT == 1 ? 0 : min(r8, G - 1))) * HD + 32 * g0 + 8 * t4;
+      constexpr int QG = INT ? NG / 2 : NG;
+      const int g0 = INT ? r8 >> 2 : 0;      // (then every second group)
+      const T* qp = q_new + ((int64_t)u * G + (INT ? 0 : min(r8, G - 1))) * HD + 32 * g0 + 8 * t4;
       float q[QG][8], most = 0.f, gs[QG];
 #pragma unroll
-      for (int g = 0; g < QG; ++g) load_new(qp + 32 * g, q[g]);
+      for (int g = 0; g < QG; ++g) load_new(qp + (INT ? 64 : 32) * g, q[g]);
 #pragma unroll
       for (int g = 0; g < QG; ++g) {
         gs[g] = 0.f;
@@ -377,36 +395,47 @@ decode_q4_kernel(int G_arg, int split, int chunk, int depth, int B, int cap, int
         gs[g] *= scale_log2;
       }
 #pragma unroll
-      for (int o = 1; o < (GT == 1 ? 32 : 4); o <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
-      // power of two that brings the largest to [2^13, 2^14)
-      const int ex = min(max(13 + 127 - (int)(__float_as_uint(most) >> 23), -100), 126);
-      const float up = __uint_as_float((uint32_t)(ex + 127) << 23), back = __uint_as_float((uint32_t)(24 - ex + 127) << 23) * scale_log2;
-      uint32_t hi[QG][4], lo[QG][4];
+      for (int o = 1; o < (INT ? 32 : 4); o <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+      const int ex = min(max((int)(__float_as_uint(most) >> 23) - 126, -90), 100);      // 2^ex is above the largest magnitude
+      if constexpr (INT) {
+        // Q = q 2^(25 - ex) as an integer; byte lo + 16 hi of a row by 16 Q_lo, its upper half 16 hi by Q_hi - 16 Q_lo
+        const float up = __uint_as_float((uint32_t)(25 - ex + 127) << 23);
+        const uint32_t sel = (uint32_t)(r8 & 3) | (uint32_t)((r8 & 3) + 4) << 4;      // this column's digit of two words
 #pragma unroll
-      for (int g = 0; g < QG; ++g)
+        for (int g = 0; g < NG; ++g) qb[g][0] = qb[g][1] = 0u;
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          const float f = x & 1 ? up * 0.0625f : up, p0 = q[g][x] * f, p1 = q[g][x + 4] * f;      // (odd channels' codes stand four bits higher)
-          const __half2 h = __floats2half2_rn(p0, p1);
-          hi[g][x] = *reinterpret_cast<const uint32_t*>(&h);
-          lo[g][x] = SPLIT_Q ? half2_of(p0 - __low2float(h), p1 - __high2float(h)) : 0u;
+        for (int g = 0; g < QG; ++g) {
+          uint32_t w[2][4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int lo = __float2int_rn(q[g][2 * i] * up), hi = __float2int_rn(q[g][2 * i + 1] * up);
+            w[0][i] = (uint32_t)(16 * lo) + 0x80808080u;          // (signed digits: a byte each, 128 too large)
+            w[1][i] = (uint32_t)(hi - 16 * lo) + 0x80808080u;
+          }
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            const uint32_t b = __byte_perm(__byte_perm(w[x][0], w[x][1], sel), __byte_perm(w[x][2], w[x][3], sel), 0x5410u) ^ 0x80808080u;
+            if (r8 < 4) qb[2 * g][x] = b;
+            else qb[2 * g + 1][x] = b;
+          }
+          qsum[g][0] = __shfl_sync(0xffffffffu, gs[g], 16 * (t4 >> 1));      // of group 2 g + t4 / 2, in the even lanes
+          if (t4 & 1) qsum[g][0] = 0.f;
+          qsum[g][1] = 0.f;
         }
-      if constexpr (GT == 1) {
-#pragma unroll
-        for (int g = 0; g < NG; ++g)
-#pragma unroll
-          for (int x = 0; x < 4; ++x) qb[g][x] = (r8 >> 1) == g ? (r8 & 1 ? lo[0][x] : hi[0][x]) : 0u;
-        q_back[0] = back;
-        qsum[0][0] = __shfl_sync(0xffffffffu, gs[0], 8 * t4);      // (row 2 t4: group t4)
-        qsum[0][1] = 0.f;
-        if (t4 >= NG) qsum[0][0] = 0.f;
+        const float back = __uint_as_float((uint32_t)(ex - 29 + 127) << 23) * scale_log2;
+        q_back[0] = t4 & 1 ? back * 65536.f : back;
+        q_back[1] = q_back[0] * 256.f;
       } else {
+        // q to [2^13, 2^14) by a power of two, as a high half and a remainder
+        const float up = __uint_as_float((uint32_t)(14 - ex + 127) << 23), back = __uint_as_float((uint32_t)(ex + 10 + 127) << 23) * scale_log2;
 #pragma unroll
         for (int g = 0; g < NG; ++g)
 #pragma unroll
           for (int x = 0; x < 4; ++x) {
-            qb[g][x] = hi[g][x];
-            if constexpr (SPLIT_Q) qr[g][x] = lo[g][x];
+            const float f = x & 1 ? up * 0.0625f : up, p0 = q[g][x] * f, p1 = q[g][x + 4] * f;      // (odd channels' codes stand four bits higher)
+            const __half2 h = __floats2half2_rn(p0, p1);
+            qb[g][x] = *reinterpret_cast<const uint32_t*>(&h);
+            if constexpr (SPLIT_Q) qr[g][x] = half2_of(p0 - __low2float(h), p1 - __high2float(h));
           }
         // (an accumulator's columns are heads 2 t4 and 2 t4 + 1; their sums are with the lanes of those columns)
 #pragma unroll
@@ -418,48 +447,44 @@ decode_q4_kernel(int G_arg, int split, int chunk, int depth, int B, int cap, int
       }
     }
 
-    // ---- the ring: the next item, its slot and the parity of its barrier; the next item to request
-    int n = tiles_in(cnt), slot = 0, next = early;
+    // ---- the ring: the next item's slot, place and the parity of its barrier; the next item to request
+    const int n = items_in(cnt);
+    int slot = 0, next = early;
     uint32_t par = 0;
+    const unsigned char* item = ring;
     auto arrived = [&]() {
-      if (!bad && !bar_wait(&full[wid][slot], par)) bad = true;
+      if (!bar_try(full_a + 8 * slot, par) && !bad && !bar_wait(full_a + 8 * slot, par)) bad = true;
     };
     auto release = [&]() {                    // every lane has read the item: its slot takes the next one
       __syncwarp();
-      if (next < 2 * n) {
-        if (lane == 0 && !bad) request(next, n, slot);
-        ++next;
-      }
-      if (++slot == depth) { slot = 0; par ^= 1; }
+      if (next < 2 * n && lane == 0 && !bad) request(next, n, slot);
+      ++next;
+      item += ITEM;
+      if (++slot == depth) { slot = 0; item = ring; par ^= 1; }
     };
-    bool fresh = true;                        // the early items were requested before the launch ahead had completed
+    int ls_item = -1;                         // the early item of K that holds the row which the launch ahead appended
+    uint32_t ls_word[2] = {0u, 0u};           // that row (lanes below CODES / 4: codes, then parameters) of K and of V
     if (n != n_alloc) {                       // fewer tokens than there is room for: what was requested early is dropped
-      const int dropped = early;
       next = 2 * n;
-      for (int j = 0; j < dropped; ++j) { arrived(); release(); }
+      for (int j = 0; j < early; ++j) { arrived(); release(); }
       next = min(depth, 2 * n);
       if (lane == 0 && !bad)
         for (int j = 0; j < next; ++j) request(j, n, (slot + j) % depth);
       __syncwarp();
-      fresh = false;
-    }
-    // the row that the launch ahead appended, for the early item that holds it (lanes below CODES / 4: codes, then parameters)
-    const int ls_item = fresh && ls >= 0 && ls != fs && ls_local >= 0 && ls_local < cnt && ls_local / Q4_TILE % Q4_WARPS == wid
-                            ? ls_local / (Q4_TILE * Q4_WARPS) : -1;
-    uint32_t ls_word[2] = {0u, 0u};
-    if (ls_item >= 0) {
+    } else if (ls >= 0 && ls != fs && ls_local >= 0 && ls_local < cnt && ls_local / Q4_ROWS % Q4_WARPS == wid) {
+      ls_item = ls_local / (Q4_ROWS * Q4_WARPS);
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
         if (lane < CODES / 4) ls_word[x] = load_fresh(reinterpret_cast<const uint32_t*>((x ? vc : kc) + (int64_t)ls_local * CODES) + lane);
         else if (lane < CODES / 4 + NG) ls_word[x] = load_fresh(reinterpret_cast<const uint32_t*>((x ? vp : kp) + (int64_t)ls_local * PARAMS) + (lane - CODES / 4));
       }
     }
-    auto patch = [&](int j, int x) {          // item j (of K: x = 0, of V: x = 1)
-      if (j == ls_item && (x ? n : 0) + j < early) {
-        unsigned char* row = ring + slot * ITEM;
-        const int r = ls_local % Q4_TILE;
-        if (lane < CODES / 4) reinterpret_cast<uint32_t*>(row + r * CODES)[lane] = ls_word[x];
-        else if (lane < CODES / 4 + NG) reinterpret_cast<uint32_t*>(row + Q4_TILE * CODES + r * PARAMS)[lane - CODES / 4] = ls_word[x];
+    auto patch = [&](int j, uint32_t word) {  // item j of the ring
+      if (j < early) {
+        unsigned char* to = ring + slot * ITEM;
+        const int r = ls_local % Q4_ROWS;
+        if (lane < CODES / 4) reinterpret_cast<uint32_t*>(to + r * CODES)[lane] = word;
+        else if (lane < CODES / 4 + NG) reinterpret_cast<uint32_t*>(to + Q4_ROWS * CODES + r * PARAMS)[lane - CODES / 4] = word;
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // (before the next bulk copy into the slot)
         __syncwarp();
       }
@@ -470,150 +495,185 @@ decode_q4_kernel(int G_arg, int split, int chunk, int depth, int B, int cap, int
     float m_run[MX];
 #pragma unroll
     for (int x = 0; x < MX; ++x) m_run[x] = -INFINITY;
-    auto k_tiles = [&](int j0, auto tiles) {
-      constexpr int N = decltype(tiles)::value;
-      uint32_t kw[N][2][KW], pr[N][2][KP];
+    // rows r0 + r8 + 8 k, k < 2 N, from tile `a0` of the item on
+    auto k_rows = [&](int r0, int a0) {
+      uint32_t kw[2 * N][KW], pr[2 * N][KP];
+      const unsigned char* codes = item + (a0 * Q4_TILE + r8) * CODES + t4 * (HD / 8);
+      const unsigned char* params = item + Q4_ROWS * CODES + (a0 * Q4_TILE + r8) * PARAMS;
 #pragma unroll
-      for (int a = 0; a < N; ++a) {
-        arrived();
-        patch(j0 + a, 0);
-        const unsigned char* tile = ring + slot * ITEM;
+      for (int k = 0; k < 2 * N; ++k) {
+        words_of(codes + 8 * k * CODES, kw[k]);
+        if constexpr (INT) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          words_of(tile + (r8 + 8 * i) * CODES + t4 * (HD / 8), kw[a][i]);
-          if constexpr (GT == 1) pr[a][i][0] = t4 < NG ? *reinterpret_cast<const uint32_t*>(tile + Q4_TILE * CODES + (r8 + 8 * i) * PARAMS + 4 * t4) : 0u;
-          else words_of(tile + Q4_TILE * CODES + (r8 + 8 * i) * PARAMS, pr[a][i]);
+          for (int f = 0; f < KP; ++f)       // of groups t4 / 2 and t4 / 2 + 2
+            pr[k][f] = *reinterpret_cast<const uint32_t*>(params + 8 * k * PARAMS + 4 * (t4 >> 1) + 8 * f);
+        } else {
+          words_of(params + 8 * k * PARAMS, pr[k]);
         }
-        release();
       }
-      float acc[N][GT > 1 ? NG : 2][4];
+      if (a0 + N == 2) release();
+      if constexpr (INT) {
+        int d[N][KP][4];                     // groups 2 f (columns 0 - 3) and 2 f + 1 (columns 4 - 7)
 #pragma unroll
-      for (int a = 0; a < N; ++a)
+        for (int g = 0; g < NG; ++g)
 #pragma unroll
-        for (int g = 0; g < (GT > 1 ? NG : 2); ++g) acc[a][g][0] = acc[a][g][1] = acc[a][g][2] = acc[a][g][3] = 0.f;
+          for (int a = 0; a < N; ++a) {
+            // words of chunks 2 t4 (first half of the lane's words) and 2 t4 + 1; a half word is a group
+            const uint32_t sel = g & 1 ? 0x7632u : 0x5410u;
+            const uint32_t xa = __byte_perm(kw[2 * a][g >> 1], kw[2 * a][KW / 2 + (g >> 1)], sel), xb = __byte_perm(kw[2 * a + 1][g >> 1], kw[2 * a + 1][KW / 2 + (g >> 1)], sel);
+            // (sums start at the float 1.5 * 2^23 as an integer: below 2^20, they are that float's low bits)
+            if (g & 1) mma_s8(d[a][g >> 1], xa, xb, xa & 0xf0f0f0f0u, xb & 0xf0f0f0f0u, qb[g][0], qb[g][1]);
+            else mma_s8(d[a][g >> 1], xa, xb, xa & 0xf0f0f0f0u, xb & 0xf0f0f0f0u, qb[g][0], qb[g][1], 0x4b400000);
+          }
+        float s[4];
 #pragma unroll
-      for (int g = 0; g < NG; ++g)
+        for (int k = 0; k < 4; ++k) {
+          s[k] = 0.f;
 #pragma unroll
-        for (int a = 0; a < N; ++a) {
-          // words of chunks 2 t4 (first half of the lane's words) and 2 t4 + 1; a half word is a group
-          const uint32_t sel = g & 1 ? 0x7632u : 0x5410u;
-          const uint32_t xa = __byte_perm(kw[a][0][g >> 1], kw[a][0][KW / 2 + (g >> 1)], sel), xb = __byte_perm(kw[a][1][g >> 1], kw[a][1][KW / 2 + (g >> 1)], sel);
-          const uint32_t ya = xa >> 8, yb = xb >> 8;
-          float(&d0)[4] = acc[a][GT > 1 ? g : 0];
-          float(&d1)[4] = acc[a][GT > 1 ? g : 1];
-          mma_f16(d0, xa & 0x000f000fu, xb & 0x000f000fu, xa & 0x00f000f0u, xb & 0x00f000f0u, qb[g][0], qb[g][1]);
-          mma_f16(d1, ya & 0x000f000fu, yb & 0x000f000fu, ya & 0x00f000f0u, yb & 0x00f000f0u, qb[g][2], qb[g][3]);
-          if constexpr (GT > 1 && SPLIT_Q) {
-            mma_f16(d0, xa & 0x000f000fu, xb & 0x000f000fu, xa & 0x00f000f0u, xb & 0x00f000f0u, qr[g][0], qr[g][1]);
-            mma_f16(d1, ya & 0x000f000fu, yb & 0x000f000fu, ya & 0x00f000f0u, yb & 0x00f000f0u, qr[g][2], qr[g][3]);
+          for (int f = 0; f < KP; ++f) {
+            const float d0 = __int_as_float(d[k >> 1][f][2 * (k & 1)]) - 12582912.f, d1 = __int_as_float(d[k >> 1][f][2 * (k & 1) + 1]) - 12582912.f;
+            s[k] = fmaf(q4_scale(pr[k][f]), fmaf(d1, q_back[1], d0 * q_back[0]), s[k]);
+            s[k] = fmaf(q4_low(pr[k][f]), qsum[f][0], s[k]);
           }
         }
+        // the four lanes of a row hold parts of its sum; lane t4 ends up with row r8 + 8 t4
+        const bool odd = t4 & 1, up = t4 & 2;
+        float a = odd ? s[1] : s[0], b = odd ? s[3] : s[2];
+        a += __shfl_xor_sync(0xffffffffu, odd ? s[0] : s[1], 1);
+        b += __shfl_xor_sync(0xffffffffu, odd ? s[2] : s[3], 1);
+        float x = (up ? b : a) + __shfl_xor_sync(0xffffffffu, up ? a : b, 2);
+        const int row = r0 + r8 + 8 * t4;
+        if (row >= cnt || row == fs_local) x = -INFINITY;      // (the incoming token's slot is the ninth warp's)
+        if (row != fs_local) logit_s[row] = x;
+        m_run[0] = fmaxf(m_run[0], x);
+      } else {
+        float acc[N][NG][4];
 #pragma unroll
-      for (int a = 0; a < N; ++a)
+        for (int g = 0; g < NG; ++g)
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const int row = tile_row(j0 + a) + r8 + 8 * i;
-          const bool live = row < cnt && row != fs_local;      // (the incoming token's slot is the ninth warp's)
-          float s[MX];
-          if constexpr (GT == 1) {
-            const float d = (acc[a][0][2 * i] + acc[a][1][2 * i]) + (acc[a][0][2 * i + 1] + acc[a][1][2 * i + 1]);
-            s[0] = fmaf(q4_scale(pr[a][i][0]) * q_back[0], d, q4_low(pr[a][i][0]) * qsum[0][0]);
-            s[0] += __shfl_xor_sync(0xffffffffu, s[0], 1);
-            s[0] += __shfl_xor_sync(0xffffffffu, s[0], 2);
-          } else {
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-              float d = 0.f, l = 0.f;
-#pragma unroll
-              for (int g = 0; g < NG; ++g) {
-                d = fmaf(q4_scale(pr[a][i][g]), acc[a][g][2 * i + x], d);
-                l = fmaf(q4_low(pr[a][i][g]), qsum[g][x], l);
-              }
-              s[x] = fmaf(d, q_back[x], l);
+          for (int a = 0; a < N; ++a) {
+            const uint32_t sel = g & 1 ? 0x7632u : 0x5410u;
+            const uint32_t xa = __byte_perm(kw[2 * a][g >> 1], kw[2 * a][KW / 2 + (g >> 1)], sel), xb = __byte_perm(kw[2 * a + 1][g >> 1], kw[2 * a + 1][KW / 2 + (g >> 1)], sel);
+            const uint32_t ya = xa >> 8, yb = xb >> 8;
+            float(&d)[4] = acc[a][g];
+            d[0] = d[1] = d[2] = d[3] = 0.f;
+            mma_f16(d, xa & 0x000f000fu, xb & 0x000f000fu, xa & 0x00f000f0u, xb & 0x00f000f0u, qb[g][0], qb[g][1]);
+            mma_f16(d, ya & 0x000f000fu, yb & 0x000f000fu, ya & 0x00f000f0u, yb & 0x00f000f0u, qb[g][2], qb[g][3]);
+            if constexpr (SPLIT_Q) {
+              mma_f16(d, xa & 0x000f000fu, xb & 0x000f000fu, xa & 0x00f000f0u, xb & 0x00f000f0u, qr[g][0], qr[g][1]);
+              mma_f16(d, ya & 0x000f000fu, yb & 0x000f000fu, ya & 0x00f000f0u, yb & 0x00f000f0u, qr[g][2], qr[g][3]);
             }
           }
 #pragma unroll
-          for (int x = 0; x < MX; ++x) {
-            if (!live) s[x] = -INFINITY;
-            const int h = GT > 1 ? 2 * t4 + x : 0;
-            if ((GT > 1 ? h < G : t4 == 0) && row != fs_local) logit_s[h * chunk + row] = s[x];
-            m_run[x] = fmaxf(m_run[x], s[x]);
+        for (int k = 0; k < 2 * N; ++k) {
+          const int row = r0 + r8 + 8 * k;
+          const bool live = row < cnt && row != fs_local;
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            float d = 0.f, l = 0.f;
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+              d = fmaf(q4_scale(pr[k][g]), acc[k >> 1][g][2 * (k & 1) + x], d);
+              l = fmaf(q4_low(pr[k][g]), qsum[g][x], l);
+            }
+            const float s = live ? fmaf(d, q_back[x], l) : -INFINITY;
+            const int h = 2 * t4 + x;
+            if (h < G && row != fs_local) logit_s[h * chunk + row] = s;
+            m_run[x] = fmaxf(m_run[x], s);
           }
         }
+      }
     };
-    {
-      int j = 0;
-      for (; j + NT <= n; j += NT) k_tiles(j, std::integral_constant<int, NT>{});
-      if (j < n) k_tiles(j, std::integral_constant<int, 1>{});
+    for (int j = 0; j < n; ++j) {
+      arrived();
+      if (j == ls_item) patch(j, ls_word[0]);
+      const int r0 = item_row(j);
+#pragma unroll 1
+      for (int a = 0; a < 2; a += N) k_rows(r0 + a * Q4_TILE, a);
     }
     // (after the wait: at most one unfinished predecessor exists while a successor sets up)
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 #pragma unroll
     for (int x = 0; x < MX; ++x) {
 #pragma unroll
-      for (int o = 4; o < 32; o <<= 1) m_run[x] = fmaxf(m_run[x], __shfl_xor_sync(0xffffffffu, m_run[x], o));
+      for (int o = INT ? 1 : 4; o < 32; o <<= 1) m_run[x] = fmaxf(m_run[x], __shfl_xor_sync(0xffffffffu, m_run[x], o));
       const int h = GT > 1 ? 2 * t4 + x : 0;
       if (r8 == 0 && (GT > 1 ? h < G : t4 == 0)) part_m[wid][h] = m_run[x];
     }
     __syncwarp();
-    if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(s32(&k_done)) : "memory");
+    if (lane == 0) bar_arrive(s32(&k_done));
 
-    // ---- O^T += V^T (p sc): A = codes (16 channels x 16 slots), B = p sc by slot and head, scaled by 2^(13 - J) to fit fp16.  J follows
-    // the largest s + log2 sc (rounded up) with a slack of 2^2; when it moves, the accumulators are rescaled (a power of two).
-    float o_acc[NG][2][4];
+    // ---- O^T += V^T (p sc): A = codes (16 channels x 16 or 32 slots), B = p sc by slot and head, scaled by a power of two to fit fp16
+    // (2^(13 - J)) or 32-bit integers (2^(29 - J)).  J follows the largest s + log2 sc (rounded up) with a slack of 2^2; when it moves,
+    // what has been summed up is rescaled (a power of two).
+    constexpr int X_TOP = INT ? 29 : 13;
+    float o_acc[NG][2][4];                   // INT: [group][0]: channels 4 r8 .. + 3 of the group, of this lane's digits
+    int o_int[INT ? NG : 1][2][4];           // sums over codes lo + 16 hi of a byte, and over 16 hi
 #pragma unroll
     for (int g = 0; g < NG; ++g)
 #pragma unroll
-      for (int i = 0; i < 2; ++i) o_acc[g][i][0] = o_acc[g][i][1] = o_acc[g][i][2] = o_acc[g][i][3] = 0.f;
-    float m_own[GT], l_run[GT], lo_run[GT][VW];      // this warp's maxima; of this lane's slots (and groups): sum of p, sum of p lo
+      for (int i = 0; i < 2; ++i) {
+        o_acc[g][i][0] = o_acc[g][i][1] = o_acc[g][i][2] = o_acc[g][i][3] = 0.f;
+        if (INT) o_int[g][i][0] = o_int[g][i][1] = o_int[g][i][2] = o_int[g][i][3] = 0;
+      }
+    const float digit0 = t4 & 1 ? 65536.f : 1.f, digit1 = digit0 * 256.f;
+    // the integer sums (below 2^31 for 33,000 slots of a warp: shared memory holds the logits of fewer) into the float ones
+    auto flush = [&]() {
+      if constexpr (INT) {
+#pragma unroll
+        for (int g = 0; g < NG; ++g)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const int h0 = o_int[g][1][2 * i], h1 = o_int[g][1][2 * i + 1];
+            o_acc[g][0][2 * i] = fmaf((float)(o_int[g][0][2 * i + 1] - h1), digit1, fmaf((float)(o_int[g][0][2 * i] - h0), digit0, o_acc[g][0][2 * i]));
+            o_acc[g][0][2 * i + 1] = fmaf((float)h1, digit1 * 0.0625f, fmaf((float)h0, digit0 * 0.0625f, o_acc[g][0][2 * i + 1]));
+            o_int[g][0][2 * i] = o_int[g][0][2 * i + 1] = o_int[g][1][2 * i] = o_int[g][1][2 * i + 1] = 0;
+          }
+      }
+    };
+    float m_own[GT], l_run[GT], lo_run[GT][PG];      // this warp's maxima; of this lane's slots (and groups): sum of p, sum of p lo
     int J[GT];
 #pragma unroll
     for (int h = 0; h < GT; ++h) {
       m_own[h] = GT == 1 || h < G ? part_m[wid][h] : -INFINITY;
       l_run[h] = 0.f;
-      J[h] = -100000000;
+      J[h] = -1000000000;
 #pragma unroll
-      for (int i = 0; i < VW; ++i) lo_run[h][i] = 0.f;
+      for (int i = 0; i < PG; ++i) lo_run[h][i] = 0.f;
     }
-    auto v_tiles = [&](int j0, auto tiles) {
-      constexpr int N = decltype(tiles)::value;
-      bool live[N];
-      float s[N][GT];
-      uint32_t vw[N][4][VW], pr[N][VW];
+    // N tiles of an item from tile a0 on.  Lane: slot `lane` of the item and all of its groups, or (N == 1) slot lane / 2 of the tile and
+    // half of the groups.
+    const int my_slot_in = N == 2 ? lane : lane >> 1, my_group = N == 2 ? 0 : (lane & 1) * VW;
+    const int x_at = (N == 2 ? (lane >> 4) * (INT ? Q4_TILE : NG * XC * Q4_TILE) : 0) + 4 * (my_slot_in & 3) + (my_slot_in >> 2 & 3);
+    auto v_rows = [&](int r0, int a0) {
+      const int row = r0 + my_slot_in;
+      float s[GT];
 #pragma unroll
-      for (int a = 0; a < N; ++a) {
-        const int row = tile_row(j0 + a) + (lane >> 1);
-        live[a] = row < cnt && row != fs_local;
+      for (int h = 0; h < GT; ++h) s[h] = GT == 1 || h < G ? logit_s[h * chunk + row] : -INFINITY;
+      uint32_t vw[N][4][VW], pr[PG];
+      words_of(item + Q4_ROWS * CODES + (a0 * Q4_TILE + my_slot_in) * PARAMS + 4 * my_group, pr);
 #pragma unroll
-        for (int h = 0; h < GT; ++h) s[a][h] = (GT == 1 || h < G) && live[a] ? logit_s[h * chunk + row] : -INFINITY;
-        arrived();
-        patch(j0 + a, 1);
-        const unsigned char* tile = ring + slot * ITEM;
-        words_of(tile + Q4_TILE * CODES + (lane >> 1) * PARAMS + (lane & 1) * VW * 4, pr[a]);
+      for (int a = 0; a < N; ++a)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) words_of(tile + (4 * i + t4) * CODES + r8 * (HD / 16), vw[a][i]);
-        release();
+        for (int i = 0; i < 4; ++i) words_of(item + ((a0 + a) * Q4_TILE + 4 * i + t4) * CODES + r8 * (HD / 16), vw[a][i]);
+      if (a0 + N == 2) release();
+      if (row >= cnt || row == fs_local) {   // (its logit is another's, or nobody's; its parameters may be anything)
+#pragma unroll
+        for (int h = 0; h < GT; ++h) s[h] = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < PG; ++i) pr[i] = 0u;
       }
-      int ev[N];                             // exponent of the largest scale, rounded up (2^-100 is the least, 0 apart)
+      float most = 0.f;                      // 126 + exponent of the largest scale, rounded up (a scale of 0 counts as 2^-96)
 #pragma unroll
-      for (int a = 0; a < N; ++a) {
-        ev[a] = -100;
-#pragma unroll
-        for (int i = 0; i < VW; ++i) {
-          if (!live[a]) pr[a][i] = 0u;
-          ev[a] = max(ev[a], (int)(pr[a][i] >> 7 & 0xffu) - 126);
-        }
-      }
+      for (int i = 0; i < PG; ++i) most = fmaxf(most, q4_scale(pr[i]));
+      const int ev = max((int)(__float_as_uint(most) >> 23), 30);
       bool moved = false;
       float f[GT];
 #pragma unroll
       for (int h = 0; h < GT; ++h) {
         f[h] = 1.f;
         if (GT == 1 || h < G) {
-          int top = -100000000;
-#pragma unroll
-          for (int a = 0; a < N; ++a) top = live[a] ? max(top, (int)ceilf(fminf(fmaxf(s[a][h], -4e6f), 4e6f)) + ev[a]) : top;
-          top = __reduce_max_sync(0xffffffffu, top);
+          const int top = __reduce_max_sync(0xffffffffu, __float2int_ru(fminf(s[h], 1e9f)) + ev);      // (-inf: the least integer)
           if (top > J[h] + 2) {
             f[h] = exp2_fast((float)(J[h] - top));
             J[h] = top;
@@ -622,62 +682,104 @@ decode_q4_kernel(int G_arg, int split, int chunk, int depth, int B, int cap, int
         }
       }
       if (moved) {
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          float fx = f[0];                   // of column 2 t4 + x
-#pragma unroll
-          for (int h = 1; h < GT; ++h) fx = (GT > 4 ? 2 * t4 + x : t4) == h ? f[h] : fx;
+        if constexpr (INT) {
+          flush();
 #pragma unroll
           for (int g = 0; g < NG; ++g)
 #pragma unroll
-            for (int i = 0; i < 2; ++i) { o_acc[g][i][x] *= fx; o_acc[g][i][2 + x] *= fx; }
+            for (int x = 0; x < 4; ++x) o_acc[g][0][x] *= f[0];
+        } else {
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            float fx = f[0];                 // of column 2 t4 + x
+#pragma unroll
+            for (int h = 1; h < GT; ++h) fx = (GT > 4 ? 2 * t4 + x : t4) == h ? f[h] : fx;
+#pragma unroll
+            for (int g = 0; g < NG; ++g)
+#pragma unroll
+              for (int i = 0; i < 2; ++i) { o_acc[g][i][x] *= fx; o_acc[g][i][2 + x] *= fx; }
+          }
         }
       }
 #pragma unroll
-      for (int a = 0; a < N; ++a)
+      for (int h = 0; h < GT; ++h)
+        if (GT == 1 || h < G) {
+          // (no live slot so far: m_own is -inf)
+          const float p = s[h] > -INFINITY ? exp2_fast(s[h] - m_own[h]) : 0.f, y = exp2_fast(s[h] - (float)(J[h] - 126 - X_TOP));
+          l_run[h] += p;
 #pragma unroll
-        for (int h = 0; h < GT; ++h)
-          if (GT == 1 || h < G) {
-            const float p = live[a] ? exp2_fast(s[a][h] - m_own[h]) : 0.f, y = live[a] ? exp2_fast(s[a][h] - (float)(J[h] - 13)) : 0.f;
-            l_run[h] += p;
+          for (int i = 0; i < PG; ++i) {
+            const float x = y * q4_scale(pr[i]);
+            lo_run[h][i] = fmaf(p, q4_low(pr[i]), lo_run[h][i]);
+            if constexpr (INT) {             // a column for each byte
+              const uint32_t X = __float2uint_rn(x);
+              unsigned char* to = xs[wid] + (my_group + i) * 4 * 2 * Q4_TILE + x_at;
 #pragma unroll
-            for (int i = 0; i < VW; ++i) {
-              const float x = y * q4_scale(pr[a][i]);
-              lo_run[h][i] = fmaf(p, q4_low(pr[a][i]), lo_run[h][i]);
+              for (int d = 0; d < 4; ++d) to[d * 2 * Q4_TILE] = (unsigned char)(X >> (8 * d));
+            } else {
               const __half hh = __float2half_rn(x), hl = __float2half_rn(x - __half2float(hh));
-              uint16_t* to = &xs[wid][a][(lane & 1) * VW + i][x_col(h, 0)][4 * (lane >> 1 & 3) + (lane >> 3)];
+              uint16_t* to = reinterpret_cast<uint16_t*>(xs[wid]) + ((my_group + i) * XC + x_col(h, 0)) * Q4_TILE + x_at;
               to[0] = __half_as_ushort(hh);
               to[(x_col(h, 1) - x_col(h, 0)) * Q4_TILE] = __half_as_ushort(hl);
             }
           }
-      __syncwarp();
-#pragma unroll
-      for (int a = 0; a < N; ++a)
-#pragma unroll
-        for (int g = 0; g < NG; ++g) {
-          const uint2 b = *reinterpret_cast<const uint2*>(&xs[wid][a][g][r8][4 * t4]);
-          const uint32_t sel = g & 1 ? 0x7632u : 0x5410u;
-          const uint32_t xa = __byte_perm(vw[a][0][g >> 1], vw[a][1][g >> 1], sel), xb = __byte_perm(vw[a][2][g >> 1], vw[a][3][g >> 1], sel);
-          const uint32_t ya = xa >> 8, yb = xb >> 8;
-          mma_f16(o_acc[g][0], xa & 0x000f000fu, xa & 0x00f000f0u, xb & 0x000f000fu, xb & 0x00f000f0u, b.x, b.y);
-          mma_f16(o_acc[g][1], ya & 0x000f000fu, ya & 0x00f000f0u, yb & 0x000f000fu, yb & 0x00f000f0u, b.x, b.y);
-          if constexpr (GT > 4) {
-            const uint2 d = *reinterpret_cast<const uint2*>(&xs[wid][a][g][8 + r8][4 * t4]);
-            mma_f16(o_acc[g][0], xa & 0x000f000fu, xa & 0x00f000f0u, xb & 0x000f000fu, xb & 0x00f000f0u, d.x, d.y);
-            mma_f16(o_acc[g][1], ya & 0x000f000fu, ya & 0x00f000f0u, yb & 0x000f000fu, yb & 0x00f000f0u, d.x, d.y);
-          }
         }
       __syncwarp();
+      if constexpr (INT) {
+        // bytes of four slots side by side: a lane's words of slots t4, t4 + 4, t4 + 8, t4 + 12, transposed
+        uint32_t tr[N][VW][4];
+#pragma unroll
+        for (int a = 0; a < N; ++a)
+#pragma unroll
+          for (int x = 0; x < VW; ++x) {
+            const uint32_t p0 = __byte_perm(vw[a][0][x], vw[a][1][x], 0x5140u), p1 = __byte_perm(vw[a][2][x], vw[a][3][x], 0x5140u);
+            const uint32_t p2 = __byte_perm(vw[a][0][x], vw[a][1][x], 0x7362u), p3 = __byte_perm(vw[a][2][x], vw[a][3][x], 0x7362u);
+            tr[a][x][0] = __byte_perm(p0, p1, 0x5410u);
+            tr[a][x][1] = __byte_perm(p0, p1, 0x7632u);
+            tr[a][x][2] = __byte_perm(p2, p3, 0x5410u);
+            tr[a][x][3] = __byte_perm(p2, p3, 0x7632u);
+          }
+        const uint32_t* xw = reinterpret_cast<const uint32_t*>(xs[wid]) + (r8 & 3) * 2 * Q4_TILE / 4 + t4;      // (columns from 4 on are not used)
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+          // rows 0 - 7: the group's first byte (channels 4 r8, + 1), rows 8 - 15: its second
+          const uint32_t b0 = xw[g * 2 * Q4_TILE], b1 = xw[g * 2 * Q4_TILE + Q4_TILE / 4];
+          const uint32_t a0 = tr[0][g >> 1][2 * (g & 1)], a1 = tr[0][g >> 1][2 * (g & 1) + 1], a2 = tr[1][g >> 1][2 * (g & 1)], a3 = tr[1][g >> 1][2 * (g & 1) + 1];
+          mma_u8(o_int[g][0], a0, a1, a2, a3, b0, b1);
+          mma_u8(o_int[g][1], a0 & 0xf0f0f0f0u, a1 & 0xf0f0f0f0u, a2 & 0xf0f0f0f0u, a3 & 0xf0f0f0f0u, b0, b1);
+        }
+      } else {
+#pragma unroll
+        for (int a = 0; a < N; ++a)
+#pragma unroll
+          for (int g = 0; g < NG; ++g) {
+            const uint16_t* xh = reinterpret_cast<const uint16_t*>(xs[wid]) + ((a * NG + g) * XC + r8) * Q4_TILE + 4 * t4;
+            const uint2 b = *reinterpret_cast<const uint2*>(xh);
+            const uint32_t sel = g & 1 ? 0x7632u : 0x5410u;
+            const uint32_t xa = __byte_perm(vw[a][0][g >> 1], vw[a][1][g >> 1], sel), xb = __byte_perm(vw[a][2][g >> 1], vw[a][3][g >> 1], sel);
+            const uint32_t ya = xa >> 8, yb = xb >> 8;
+            mma_f16(o_acc[g][0], xa & 0x000f000fu, xa & 0x00f000f0u, xb & 0x000f000fu, xb & 0x00f000f0u, b.x, b.y);
+            mma_f16(o_acc[g][1], ya & 0x000f000fu, ya & 0x00f000f0u, yb & 0x000f000fu, yb & 0x00f000f0u, b.x, b.y);
+            if constexpr (GT > 4) {
+              const uint2 d = *reinterpret_cast<const uint2*>(xh + 8 * Q4_TILE);
+              mma_f16(o_acc[g][0], xa & 0x000f000fu, xa & 0x00f000f0u, xb & 0x000f000fu, xb & 0x00f000f0u, d.x, d.y);
+              mma_f16(o_acc[g][1], ya & 0x000f000fu, ya & 0x00f000f0u, yb & 0x000f000fu, yb & 0x00f000f0u, d.x, d.y);
+            }
+          }
+      }
+      __syncwarp();
     };
-    {
-      int j = 0;
-      for (; j + NT <= n; j += NT) v_tiles(j, std::integral_constant<int, NT>{});
-      if (j < n) v_tiles(j, std::integral_constant<int, 1>{});
+    for (int j = 0; j < n; ++j) {
+      arrived();
+      if (j == ls_item) patch(n + j, ls_word[1]);
+      const int r0 = item_row(j);
+#pragma unroll 1
+      for (int a = 0; a < 2; a += N) v_rows(r0 + a * Q4_TILE, a);
     }
     fetch(tid);
     // ---- the warp's partial, relative to the CTA's maximum: sums of p (even lanes) and of p lo, and O^T with its constant factors
     // (codes in odd channels stand four bits higher), into the ring
-    if (!bad && !bar_wait(&k_done, 0)) bad = true;
+    if (!bad && !bar_wait(s32(&k_done), 0)) bad = true;
     __syncwarp();
     float fo[2] = {0.f, 0.f};                // of this lane's columns
 #pragma unroll
@@ -687,35 +789,41 @@ decode_q4_kernel(int G_arg, int split, int chunk, int depth, int B, int cap, int
 #pragma unroll
         for (int k = 0; k <= Q4_WARPS; ++k) m = fmaxf(m, part_m[k][h]);
         const bool any = m_own[h] > -INFINITY;
-        const float fm = any ? exp2_fast(m_own[h] - m) : 0.f, fj = any ? exp2_fast((float)(J[h] + 11) - m) : 0.f;
+        const float fm = any ? exp2_fast(m_own[h] - m) : 0.f, fj = any ? exp2_fast((float)(J[h] - 126 - X_TOP + (INT ? 0 : 24)) - m) : 0.f;
 #pragma unroll
         for (int x = 0; x < 2; ++x)
           if ((GT > 4 ? 2 * t4 + x : t4) == h) fo[x] = fj;
 #pragma unroll
-        for (int o = 2; o < 32; o <<= 1) {
+        for (int o = N == 2 ? 1 : 2; o < 32; o <<= 1) {
           l_run[h] += __shfl_xor_sync(0xffffffffu, l_run[h], o);
 #pragma unroll
-          for (int i = 0; i < VW; ++i) lo_run[h][i] += __shfl_xor_sync(0xffffffffu, lo_run[h][i], o);
+          for (int i = 0; i < PG; ++i) lo_run[h][i] += __shfl_xor_sync(0xffffffffu, lo_run[h][i], o);
         }
-        if (lane < 2) {
+        if (lane < (N == 2 ? 1 : 2)) {
           if (lane == 0) part_l[wid][h] = l_run[h] * fm;
 #pragma unroll
-          for (int i = 0; i < VW; ++i) part_lo[wid][h][lane * VW + i] = lo_run[h][i] * fm;
+          for (int i = 0; i < PG; ++i) part_lo[wid][h][my_group + i] = lo_run[h][i] * fm;
         }
       }
+    flush();
     float* po = reinterpret_cast<float*>(ring);
 #pragma unroll
     for (int x = 0; x < (GT > 4 ? 2 : 1); ++x) {
       const int h = GT > 4 ? 2 * t4 + x : t4;
-      if (h < G) {
 #pragma unroll
-        for (int g = 0; g < NG; ++g) {
-          float o[4];
+      for (int g = 0; g < NG; ++g) {
+        float o[4];
 #pragma unroll
-          for (int i = 0; i < 4; ++i)        // channel 4 r8 + i of the group; the remainder's column beside it
-            o[i] = (GT > 4 ? o_acc[g][i >> 1][2 * (i & 1) + x] : o_acc[g][i >> 1][2 * (i & 1)] + o_acc[g][i >> 1][2 * (i & 1) + 1]) * (i & 1 ? fo[x] * 0.0625f : fo[x]);
-          *reinterpret_cast<float4*>(po + h * HD + 32 * g + 4 * r8) = make_float4(o[0], o[1], o[2], o[3]);
+        for (int i = 0; i < 4; ++i) {        // channel 4 r8 + i of the group
+          if constexpr (INT) {
+            o[i] = o_acc[g][0][i] + __shfl_xor_sync(0xffffffffu, o_acc[g][0][i], 1);      // (the upper digits' columns)
+            o[i] *= fo[0];
+          } else {                           // the remainder's column beside the head's; codes in odd channels stand four bits higher
+            o[i] = GT > 4 ? o_acc[g][i >> 1][2 * (i & 1) + x] : o_acc[g][i >> 1][2 * (i & 1)] + o_acc[g][i >> 1][2 * (i & 1) + 1];
+            o[i] *= i & 1 ? fo[x] * 0.0625f : fo[x];
+          }
         }
+        if (h < G) *reinterpret_cast<float4*>(po + h * HD + 32 * g + 4 * r8) = make_float4(o[0], o[1], o[2], o[3]);
       }
     }
   }
@@ -742,7 +850,7 @@ decode_q4_kernel(int G_arg, int split, int chunk, int depth, int B, int cap, int
     const int dst = ch >> slice_log2;
     send(at_rank(s32(&xo[(rank * G + h) * slice + (ch & (slice - 1))]), dst), a, at_rank(s32(&ex_bar), dst));
   }
-  if (!bar_wait(&ex_bar, 0)) bad = true;
+  if (!bar_wait(s32(&ex_bar), 0)) bad = true;
 
   // ---- every CTA: the unit's normaliser (all data is local now) and its slice of the output
   float m_all = -INFINITY, inv_all = 0.f;      // of the one head
@@ -848,7 +956,7 @@ decode_q4_kernel(int G_arg, int split, int chunk, int depth, int B, int cap, int
     int out_slot = hi, left = hi, ev = -1;                         // not evicting: the cache grows
     bool write = lane == 0;
     if (evicting) {
-      if (!bar_wait(&cand_bar, 0)) bad = true;
+      if (!bar_wait(s32(&cand_bar), 0)) bad = true;
       Q4Candidate best{Q4_NO_KEY, -1, -1};
       for (int i = lane; i < split * Q4_WARPS; i += 32)
         if (cand[i].key < best.key) best = cand[i];
@@ -888,15 +996,15 @@ cudaError_t launch_gt(int units, int G, int B, int F, int R, int window, int nor
   const int cap = cache_capacity(B), sms = device_sm_count();
   constexpr int ITEM = q4_item<HD>;
   // Static arrays and what the system takes, rounded up; half of an SM's shared memory and all of it.
-  constexpr size_t fixed = (GT > 4 ? 27 : GT > 1 ? 23 : 21) * 1024, half_sm = 113 * 1024 - fixed, whole_sm = 226 * 1024 - fixed;
-  auto chunk_of = [&](int split) { return ((cap + split - 1) / split + Q4_TILE - 1) / Q4_TILE * Q4_TILE; };
+  constexpr size_t fixed = (GT > 4 ? 27 : GT > 1 ? 23 : 9) * 1024, half_sm = 113 * 1024 - fixed, whole_sm = 226 * 1024 - fixed;
+  auto chunk_of = [&](int split) { return ((cap + split - 1) / split + Q4_ROWS - 1) / Q4_ROWS * Q4_ROWS; };
   // a ring takes the warp's partial output in the end
   const int least = (G * HD * 4 + ITEM - 1) / ITEM > 2 ? (G * HD * 4 + ITEM - 1) / ITEM : 2;
   auto bytes = [&](int split, int depth) { return (size_t)Q4_WARPS * depth * ITEM + (size_t)G * HD * 4 + (size_t)G * chunk_of(split) * 4; };
   int split = 1;
-  while (split < Q4_SPLIT && units * split * 2 <= Q4_FILL * sms && cap / (split * 2) >= 4 * Q4_TILE) split *= 2;
+  while (split < Q4_SPLIT && units * split * 2 <= Q4_FILL * sms && cap / (split * 2) >= 2 * Q4_ROWS) split *= 2;
   while (split < Q4_SPLIT && bytes(split, least) > whole_sm) split *= 2;
-  const int chunk = chunk_of(split), per_warp = (chunk / Q4_TILE + Q4_WARPS - 1) / Q4_WARPS;
+  const int chunk = chunk_of(split), per_warp = (chunk / Q4_ROWS + Q4_WARPS - 1) / Q4_WARPS;
   int depth = 2 * per_warp;
   depth = depth < least ? least : depth > Q4_DEPTH ? Q4_DEPTH : depth;
   const size_t limit = bytes(split, least) <= half_sm ? half_sm : whole_sm;
