@@ -33,9 +33,11 @@ constexpr int Q4_WARPS = 8;            // that take slots
 constexpr int Q4_WORKERS = Q4_WARPS * 32, Q4_THREADS = Q4_WORKERS + 32;
 constexpr int Q4_TILE = 16;            // slots of an MMA tile
 constexpr int Q4_ROWS = 32;            // slots of a warp at a time: an item of its ring
-constexpr int Q4_SPLIT = 8;            // CTAs of a unit at most
+constexpr int Q4_SPLIT = 16;           // CTAs of a unit at most
 constexpr int Q4_HEADS = 8;            // query heads of a unit at most (columns of the MMA tiles)
+constexpr int Q4_EXTRA = 8;            // slots beyond the tiles that the ninth warp takes at most
 constexpr int Q4_DEPTH = 8;            // items in a warp's ring at most
+constexpr int Q4_FLUSH = 64 * Q4_ROWS;      // 255 * 15 * 257 * 2048 < 2^31
 constexpr float Q4_LOG2E = 1.4426950408889634f;
 constexpr unsigned long long Q4_NO_KEY = ~0ull;
 
@@ -113,6 +115,11 @@ __device__ __forceinline__ float exp2_fast(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+__device__ __forceinline__ float max_of(float x) {      // over the warp
+  float y;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
+  return y;
+}
 __device__ __forceinline__ uint32_t half2_of(float lo, float hi) {
   const __half2 h = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&h);
@@ -178,12 +185,12 @@ __device__ __forceinline__ unsigned long long min_key(unsigned long long key) {
 // GT: 1 - one query head per cache; 4 - two to four, the columns of the second product are the heads' high halves and then the
 // remainders; 8 - five to eight, a column a head and two products.
 // Dynamic shared memory: rings [8][depth][tile], which take the warps' partial outputs in the end | the ninth partial [G][HD] |
-// logits [G][chunk].
+// logits [G][ld].
 template <int HD> constexpr int q4_item = Q4_ROWS * (HD / 2 + HD / 8);      // bytes of an item: codes, then parameters
 
 template <typename T, int HD, bool WINDOWED, int GT>
 __global__ void __launch_bounds__(Q4_THREADS, 2)
-decode_q4_kernel(int G_arg, int split, int chunk, int depth, int B, int cap, int F, int R, int w, int norm, float scale_log2, vatp_cache_q4 c, const T* q_new,
+decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int cap, int F, int R, int w, int norm, float scale_log2, vatp_cache_q4 c, const T* q_new,
                  const T* k_new, const T* v_new, T* out, int32_t* evicted, int32_t* dev_status) {
   constexpr int NG = HD / 32, KW = HD / 32, VW = HD / 64;       // groups of a row; 32-bit words of a lane in a K row and a V row
   constexpr bool INT = GT == 1;                                 // products in integers (see the top)
@@ -215,7 +222,8 @@ decode_q4_kernel(int G_arg, int split, int chunk, int depth, int B, int cap, int
   const int tid = threadIdx.x, lane = tid & 31, wid = __shfl_sync(0xffffffffu, tid >> 5, 0);
   const int r8 = lane >> 2, t4 = lane & 3;
   const int u = blockIdx.x / split;
-  const int s0 = min(rank * chunk, cap), rows_alloc = min(chunk, cap - s0);      // this CTA's slots of the unit
+  // this CTA's slots of the unit: those of the tiles, and in the last CTA up to Q4_EXTRA more (see launch_gt)
+  const int s0 = min(rank * chunk, cap), rows_alloc = min(chunk, cap - s0), rows_all = rank == split - 1 ? cap - s0 : rows_alloc;
   const int64_t base = (int64_t)u * cap + s0;
   if (tid < Q4_WARPS * Q4_DEPTH) bar_init(&full[0][tid], 1);
   if (tid == Q4_WORKERS) {
@@ -228,7 +236,7 @@ decode_q4_kernel(int G_arg, int split, int chunk, int depth, int B, int cap, int
     bar_expect(s32(&ex_bar), (uint32_t)(8 * G * split + 4 * G * HD));
     if (rank == 0) bar_expect(s32(&cand_bar), (uint32_t)(split * Q4_WARPS * sizeof(Q4Candidate)));
   }
-  if (wid < Q4_WARPS)      // (columns without a head stay 0)
+  if (!INT && wid < Q4_WARPS)      // (columns without a head stay 0)
     for (int i = lane; i < XS / 4; i += 32) reinterpret_cast<uint32_t*>(xs[wid])[i] = 0u;
   __syncthreads();
   // Another CTA's shared memory may only be written once that CTA runs and its barriers are armed: everyone arrives here and
@@ -248,11 +256,11 @@ decode_q4_kernel(int G_arg, int split, int chunk, int depth, int B, int cap, int
   const uint32_t ring_a = s32(ring), full_a = s32(&full[wid < Q4_WARPS ? wid : 0][0]);
   auto request = [&](int j, int n, int slot) {      // one lane: item j into ring slot `slot`
     const bool is_v = j >= n;
-    const int r0 = item_row(is_v ? j - n : j), rows = min(Q4_ROWS, rows_alloc - r0);      // (a multiple of eight)
+    const unsigned r0 = item_row(is_v ? j - n : j), rows = min(Q4_ROWS, rows_alloc - (int)r0);      // (a multiple of eight)
     const uint32_t bar = full_a + 8 * slot, dst = ring_a + slot * ITEM;
-    bar_expect(bar, (uint32_t)(rows * (CODES + PARAMS)));
-    bulk_load(dst, (is_v ? vc : kc) + (int64_t)r0 * CODES, rows * CODES, bar);
-    bulk_load(dst + Q4_ROWS * CODES, (is_v ? vp : kp) + (int64_t)r0 * PARAMS, rows * PARAMS, bar);
+    bar_expect(bar, rows * (CODES + PARAMS));
+    bulk_load(dst, (is_v ? vc : kc) + (uint64_t)r0 * CODES, rows * CODES, bar);
+    bulk_load(dst + Q4_ROWS * CODES, (is_v ? vp : kp) + (uint64_t)r0 * PARAMS, rows * PARAMS, bar);
   };
   const int n_alloc = wid < Q4_WARPS ? items_in(rows_alloc) : 0, early = min(depth, 2 * n_alloc);
   if (lane == 0)
@@ -280,11 +288,32 @@ decode_q4_kernel(int G_arg, int split, int chunk, int depth, int B, int cap, int
         if (h < G) load_new(q_new + ((int64_t)u * G + h) * HD + 4 * lane, qv[h]);
     }
     const int len = min(max(len_m, 0), cap - 1), fs_local = min(max(fs_m, 0), cap - 1) - s0;
-    const int cnt = max(min(len + 1 - s0, rows_alloc), 0);
+    const int cnt = max(min(len + 1 - s0, rows_all), 0);
     const bool owns = fs_local >= 0 && fs_local < cnt;
-    float s[GT];
+    float m[GT], l[GT], o[GT][4];
 #pragma unroll
-    for (int h = 0; h < GT; ++h) s[h] = -INFINITY;
+    for (int h = 0; h < GT; ++h) {
+      m[h] = -INFINITY;
+      l[h] = o[h][0] = o[h][1] = o[h][2] = o[h][3] = 0.f;
+    }
+    auto take = [&](int row) {             // the row whose values are in kv: logits, running maxima, sums and outputs
+#pragma unroll
+      for (int h = 0; h < GT; ++h) {
+        if (GT > 1 && h >= G) continue;
+        float s = 0.f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s = fmaf(qv[h][e], kv[0][e], s);      // (zeros from lane HD / 4 on)
+#pragma unroll
+        for (int x = 16; x; x >>= 1) s += __shfl_xor_sync(0xffffffffu, s, x);
+        s *= scale_log2;
+        if (lane == 0) logit_s[h * ld + row] = s;
+        const float m_new = fmaxf(m[h], s), f = exp2_fast(m[h] - m_new), p = exp2_fast(s - m_new);
+        m[h] = m_new;
+        l[h] = fmaf(l[h], f, p);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[h][e] = fmaf(o[h][e], f, p * kv[1][e]);
+      }
+    };
     if (owns) {
       float nv = 0.f;
 #pragma unroll
@@ -302,21 +331,9 @@ decode_q4_kernel(int G_arg, int split, int chunk, int depth, int B, int cap, int
 #pragma unroll
         for (int e = 0; e < 4; ++e) kv[x][e] = fmaf((float)(code >> (4 * e) & 15u), q4_scale(par), q4_low(par));
       }
+      take(fs_local);
 #pragma unroll
-      for (int h = 0; h < GT; ++h) {
-        if (GT > 1 && h >= G) continue;
-        float d = 0.f;
-        if (lane < HD / 4) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) d = fmaf(qv[h][e], kv[0][e], d);
-        }
-#pragma unroll
-        for (int o = 16; o; o >>= 1) d += __shfl_xor_sync(0xffffffffu, d, o);
-        s[h] = d * scale_log2;
-        if (lane == 0) logit_s[h * chunk + fs_local] = s[h];
-      }
-#pragma unroll
-      for (int o = 16; o; o >>= 1) nv = norm_merge(norm, nv, __shfl_xor_sync(0xffffffffu, nv, o));
+      for (int x = 16; x; x >>= 1) nv = norm_merge(norm, nv, __shfl_xor_sync(0xffffffffu, nv, x));
       nv = norm_finish(norm, nv);
       if (lane == 0) {
         new_norm_s = nv;
@@ -324,10 +341,25 @@ decode_q4_kernel(int G_arg, int split, int chunk, int depth, int B, int cap, int
         c.state.pos[base + fs_local] = t;
       }
     }
+    for (int row = rows_alloc; row < cnt; ++row) {
+      if (row == fs_local) continue;
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        uint32_t code = 0, par = 0;
+        if (lane < HD / 4) {
+          const int b = q4_byte<HD>(lane >> 3, lane & 7);
+          code = load_fresh(reinterpret_cast<const uint32_t*>((x ? vc : kc) + (int64_t)row * CODES + (b & ~3))) >> (8 * (b & 2));
+          par = load_fresh(reinterpret_cast<const uint32_t*>((x ? vp : kp) + (int64_t)row * PARAMS) + (lane >> 3));
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) kv[x][e] = fmaf((float)(code >> (4 * e) & 15u), q4_scale(par), q4_low(par));
+      }
+      take(row);
+    }
     if (lane == 0) {
 #pragma unroll
       for (int h = 0; h < GT; ++h)
-        if (GT == 1 || h < G) part_m[Q4_WARPS][h] = s[h];
+        if (GT == 1 || h < G) part_m[Q4_WARPS][h] = m[h];
       bar_arrive(s32(&k_done));
     }
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -335,18 +367,18 @@ decode_q4_kernel(int G_arg, int split, int chunk, int depth, int B, int cap, int
 #pragma unroll
     for (int h = 0; h < GT; ++h) {
       if (GT > 1 && h >= G) continue;
-      float m = s[h];
+      float top = m[h];
 #pragma unroll
-      for (int k = 0; k < Q4_WARPS; ++k) m = fmaxf(m, part_m[k][h]);
-      const float f = owns ? exp2_fast(s[h] - m) : 0.f;
-      if (lane == 0) part_l[Q4_WARPS][h] = f;
-      if (lane < HD / 4) *reinterpret_cast<float4*>(new_o + h * HD + 4 * lane) = make_float4(kv[1][0] * f, kv[1][1] * f, kv[1][2] * f, kv[1][3] * f);
+      for (int k = 0; k < Q4_WARPS; ++k) top = fmaxf(top, part_m[k][h]);
+      const float f = m[h] > -INFINITY ? exp2_fast(m[h] - top) : 0.f;
+      if (lane == 0) part_l[Q4_WARPS][h] = l[h] * f;
+      if (lane < HD / 4) *reinterpret_cast<float4*>(new_o + h * HD + 4 * lane) = make_float4(o[h][0] * f, o[h][1] * f, o[h][2] * f, o[h][3] * f);
     }
   }
 
   const int len = min(max(len_m, 0), cap - 1), fs = min(max(fs_m, 0), cap - 1);
   const int hi = len + 1;                // slots [0, hi) are live once the new token is in
-  const int cnt = max(min(hi - s0, rows_alloc), 0);
+  const int cnt = max(min(hi - s0, rows_all), 0), cnt_t = min(cnt, rows_alloc);      // live slots, and those in tiles
   const int fs_local = fs - s0, ls_local = ls - s0;
   constexpr int SB = 2;                  // slots of a thread whose state is in registers at a time
   float old_r[SB], norm_r[SB];
@@ -448,7 +480,7 @@ decode_q4_kernel(int G_arg, int split, int chunk, int depth, int B, int cap, int
     }
 
     // ---- the ring: the next item's slot, place and the parity of its barrier; the next item to request
-    const int n = items_in(cnt);
+    const int n = items_in(cnt_t);
     int slot = 0, next = early;
     uint32_t par = 0;
     const unsigned char* item = ring;
@@ -471,7 +503,7 @@ decode_q4_kernel(int G_arg, int split, int chunk, int depth, int B, int cap, int
       if (lane == 0 && !bad)
         for (int j = 0; j < next; ++j) request(j, n, (slot + j) % depth);
       __syncwarp();
-    } else if (ls >= 0 && ls != fs && ls_local >= 0 && ls_local < cnt && ls_local / Q4_ROWS % Q4_WARPS == wid) {
+    } else if (ls >= 0 && ls != fs && ls_local >= 0 && ls_local < cnt_t && ls_local / Q4_ROWS % Q4_WARPS == wid) {
       ls_item = ls_local / (Q4_ROWS * Q4_WARPS);
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
@@ -543,8 +575,8 @@ decode_q4_kernel(int G_arg, int split, int chunk, int depth, int B, int cap, int
         b += __shfl_xor_sync(0xffffffffu, odd ? s[2] : s[3], 1);
         float x = (up ? b : a) + __shfl_xor_sync(0xffffffffu, up ? a : b, 2);
         const int row = r0 + r8 + 8 * t4;
-        if (row >= cnt || row == fs_local) x = -INFINITY;      // (the incoming token's slot is the ninth warp's)
-        if (row != fs_local) logit_s[row] = x;
+        if (row >= cnt_t || row == fs_local) x = -INFINITY;      // (the incoming token's slot is the ninth warp's)
+        if (row < cnt_t && row != fs_local) logit_s[row] = x;
         m_run[0] = fmaxf(m_run[0], x);
       } else {
         float acc[N][NG][4];
@@ -567,7 +599,7 @@ decode_q4_kernel(int G_arg, int split, int chunk, int depth, int B, int cap, int
 #pragma unroll
         for (int k = 0; k < 2 * N; ++k) {
           const int row = r0 + r8 + 8 * k;
-          const bool live = row < cnt && row != fs_local;
+          const bool live = row < cnt_t && row != fs_local;
 #pragma unroll
           for (int x = 0; x < 2; ++x) {
             float d = 0.f, l = 0.f;
@@ -578,7 +610,7 @@ decode_q4_kernel(int G_arg, int split, int chunk, int depth, int B, int cap, int
             }
             const float s = live ? fmaf(d, q_back[x], l) : -INFINITY;
             const int h = 2 * t4 + x;
-            if (h < G && row != fs_local) logit_s[h * chunk + row] = s;
+            if (h < G && live) logit_s[h * ld + row] = s;
             m_run[x] = fmaxf(m_run[x], s);
           }
         }
@@ -616,21 +648,6 @@ decode_q4_kernel(int G_arg, int split, int chunk, int depth, int B, int cap, int
         o_acc[g][i][0] = o_acc[g][i][1] = o_acc[g][i][2] = o_acc[g][i][3] = 0.f;
         if (INT) o_int[g][i][0] = o_int[g][i][1] = o_int[g][i][2] = o_int[g][i][3] = 0;
       }
-    const float digit0 = t4 & 1 ? 65536.f : 1.f, digit1 = digit0 * 256.f;
-    // the integer sums (below 2^31 for 33,000 slots of a warp: shared memory holds the logits of fewer) into the float ones
-    auto flush = [&]() {
-      if constexpr (INT) {
-#pragma unroll
-        for (int g = 0; g < NG; ++g)
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const int h0 = o_int[g][1][2 * i], h1 = o_int[g][1][2 * i + 1];
-            o_acc[g][0][2 * i] = fmaf((float)(o_int[g][0][2 * i + 1] - h1), digit1, fmaf((float)(o_int[g][0][2 * i] - h0), digit0, o_acc[g][0][2 * i]));
-            o_acc[g][0][2 * i + 1] = fmaf((float)h1, digit1 * 0.0625f, fmaf((float)h0, digit0 * 0.0625f, o_acc[g][0][2 * i + 1]));
-            o_int[g][0][2 * i] = o_int[g][0][2 * i + 1] = o_int[g][1][2 * i] = o_int[g][1][2 * i + 1] = 0;
-          }
-      }
-    };
     float m_own[GT], l_run[GT], lo_run[GT][PG];      // this warp's maxima; of this lane's slots (and groups): sum of p, sum of p lo
     int J[GT];
 #pragma unroll
@@ -645,19 +662,21 @@ decode_q4_kernel(int G_arg, int split, int chunk, int depth, int B, int cap, int
     // half of the groups.
     const int my_slot_in = N == 2 ? lane : lane >> 1, my_group = N == 2 ? 0 : (lane & 1) * VW;
     const int x_at = (N == 2 ? (lane >> 4) * (INT ? Q4_TILE : NG * XC * Q4_TILE) : 0) + 4 * (my_slot_in & 3) + (my_slot_in >> 2 & 3);
-    auto v_rows = [&](int r0, int a0) {
-      const int row = r0 + my_slot_in;
+    bool last = n == 0;                      // (INT: one round more, which only takes the integer sums over)
+    const float digits = t4 & 1 ? 65536.f : 1.f;
+    auto v_rows = [&](int j, int a0) {
+      const int row = item_row(j) + a0 * Q4_TILE + my_slot_in;
+      const bool live = row < cnt_t && row != fs_local && !last;
       float s[GT];
+      uint32_t pr[PG];
+      bool moved = last || (INT && j % (Q4_FLUSH / Q4_ROWS) == Q4_FLUSH / Q4_ROWS - 1);
+      float f[GT];
+      if (!last) {
 #pragma unroll
-      for (int h = 0; h < GT; ++h) s[h] = GT == 1 || h < G ? logit_s[h * chunk + row] : -INFINITY;
-      uint32_t vw[N][4][VW], pr[PG];
-      words_of(item + Q4_ROWS * CODES + (a0 * Q4_TILE + my_slot_in) * PARAMS + 4 * my_group, pr);
-#pragma unroll
-      for (int a = 0; a < N; ++a)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) words_of(item + ((a0 + a) * Q4_TILE + 4 * i + t4) * CODES + r8 * (HD / 16), vw[a][i]);
-      if (a0 + N == 2) release();
-      if (row >= cnt || row == fs_local) {   // (its logit is another's, or nobody's; its parameters may be anything)
+        for (int h = 0; h < GT; ++h) s[h] = GT == 1 || h < G ? logit_s[h * ld + row] : -INFINITY;
+        words_of(item + Q4_ROWS * CODES + (a0 * Q4_TILE + my_slot_in) * PARAMS + 4 * my_group, pr);
+      }
+      if (!live) {                           // (its logit is another's, or nobody's; its parameters may be anything)
 #pragma unroll
         for (int h = 0; h < GT; ++h) s[h] = -INFINITY;
 #pragma unroll
@@ -667,8 +686,6 @@ decode_q4_kernel(int G_arg, int split, int chunk, int depth, int B, int cap, int
 #pragma unroll
       for (int i = 0; i < PG; ++i) most = fmaxf(most, q4_scale(pr[i]));
       const int ev = max((int)(__float_as_uint(most) >> 23), 30);
-      bool moved = false;
-      float f[GT];
 #pragma unroll
       for (int h = 0; h < GT; ++h) {
         f[h] = 1.f;
@@ -681,13 +698,18 @@ decode_q4_kernel(int G_arg, int split, int chunk, int depth, int B, int cap, int
           }
         }
       }
-      if (moved) {
+      if (moved && (!INT || j > 0)) {        // (INT, j = 0: nothing has been summed up)
         if constexpr (INT) {
-          flush();
+          // The integer sums go into the float ones: a lane's two digits make one number, below 2^31 for up to Q4_FLUSH slots of a warp.
 #pragma unroll
           for (int g = 0; g < NG; ++g)
 #pragma unroll
-            for (int x = 0; x < 4; ++x) o_acc[g][0][x] *= f[0];
+            for (int i = 0; i < 2; ++i) {
+              const int h0 = o_int[g][1][2 * i], h1 = o_int[g][1][2 * i + 1];
+              o_acc[g][0][2 * i] = f[0] * fmaf((float)((o_int[g][0][2 * i] - h0) + 256 * (o_int[g][0][2 * i + 1] - h1)), digits, o_acc[g][0][2 * i]);
+              o_acc[g][0][2 * i + 1] = f[0] * fmaf((float)((h0 >> 4) + 16 * h1), digits, o_acc[g][0][2 * i + 1]);
+              o_int[g][0][2 * i] = o_int[g][0][2 * i + 1] = o_int[g][1][2 * i] = o_int[g][1][2 * i + 1] = 0;
+            }
         } else {
 #pragma unroll
           for (int x = 0; x < 2; ++x) {
@@ -701,6 +723,12 @@ decode_q4_kernel(int G_arg, int split, int chunk, int depth, int B, int cap, int
           }
         }
       }
+      if (last) return;
+      uint32_t vw[N][4][VW];
+#pragma unroll
+      for (int a = 0; a < N; ++a)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) words_of(item + ((a0 + a) * Q4_TILE + 4 * i + t4) * CODES + r8 * (HD / 16), vw[a][i]);
 #pragma unroll
       for (int h = 0; h < GT; ++h)
         if (GT == 1 || h < G) {
@@ -724,7 +752,8 @@ decode_q4_kernel(int G_arg, int split, int chunk, int depth, int B, int cap, int
             }
           }
         }
-      __syncwarp();
+      if (a0 + N == 2) release();            // (with a barrier of the warp)
+      else __syncwarp();
       if constexpr (INT) {
         // bytes of four slots side by side: a lane's words of slots t4, t4 + 4, t4 + 8, t4 + 12, transposed
         uint32_t tr[N][VW][4];
@@ -769,12 +798,15 @@ decode_q4_kernel(int G_arg, int split, int chunk, int depth, int B, int cap, int
       }
       __syncwarp();
     };
-    for (int j = 0; j < n; ++j) {
-      arrived();
-      if (j == ls_item) patch(n + j, ls_word[1]);
-      const int r0 = item_row(j);
+    for (int j = 0; !last; ++j) {
+      if (j < n) {
+        arrived();
+        if (j == ls_item) patch(n + j, ls_word[1]);
+      }
+      last = j == n;
+      if (last && !INT) break;
 #pragma unroll 1
-      for (int a = 0; a < 2; a += N) v_rows(r0 + a * Q4_TILE, a);
+      for (int a = 0; a < 2; a += N) v_rows(j, a);
     }
     fetch(tid);
     // ---- the warp's partial, relative to the CTA's maximum: sums of p (even lanes) and of p lo, and O^T with its constant factors
@@ -805,7 +837,6 @@ decode_q4_kernel(int G_arg, int split, int chunk, int depth, int B, int cap, int
           for (int i = 0; i < PG; ++i) part_lo[wid][h][my_group + i] = lo_run[h][i] * fm;
         }
       }
-    flush();
     float* po = reinterpret_cast<float*>(ring);
 #pragma unroll
     for (int x = 0; x < (GT > 4 ? 2 : 1); ++x) {
@@ -852,50 +883,33 @@ decode_q4_kernel(int G_arg, int split, int chunk, int depth, int B, int cap, int
   }
   if (!bar_wait(s32(&ex_bar), 0)) bad = true;
 
-  // ---- every CTA: the unit's normaliser (all data is local now) and its slice of the output
-  float m_all = -INFINITY, inv_all = 0.f;      // of the one head
-  auto join = [&](int h, float (&fr)[Q4_SPLIT]) {
-    float2 ml[Q4_SPLIT];
-    float L = 0.f;
-    m_all = -INFINITY;
+  // ---- every CTA: the unit's normaliser (all data is local now) and its slice of the output.  Lane r has CTA r's maximum and sum.
+  float m_all = -INFINITY, inv_all = 0.f, fr = 0.f;      // of the one head (all warps), or of head `wid`
+  if (GT == 1 || wid < G) {
+    const float2 ml = lane < split ? ex_ml[lane][GT == 1 ? 0 : wid] : make_float2(-INFINITY, 0.f);
+    m_all = max_of(ml.x);
+    fr = ml.x > -INFINITY ? exp2_fast(ml.x - m_all) : 0.f;
+    float L = ml.y * fr;
 #pragma unroll
-    for (int r = 0; r < Q4_SPLIT; ++r) {
-      ml[r] = r < split ? ex_ml[r][h] : make_float2(-INFINITY, 0.f);
-      m_all = fmaxf(m_all, ml[r].x);
-    }
-#pragma unroll
-    for (int r = 0; r < Q4_SPLIT; ++r) {
-      fr[r] = ml[r].x > -INFINITY ? exp2_fast(ml[r].x - m_all) : 0.f;
-      L = fmaf(ml[r].y, fr[r], L);
-    }
-    inv_all = 1.f / L;
-  };
+    for (int o = Q4_SPLIT / 2; o; o >>= 1) L += __shfl_xor_sync(0xffffffffu, L, o);
+    inv_all = 1.f / __shfl_sync(0xffffffffu, L, 0);
+  }
   if constexpr (GT == 1) {
-    float fr[Q4_SPLIT];
-    join(0, fr);
-    if (tid < slice) {
+    if (wid * 32 < slice) {
       float a = 0.f;
-#pragma unroll
-      for (int r = 0; r < Q4_SPLIT; ++r)
-        if (r < split) a = fmaf(xo[r * slice + tid], fr[r], a);
-      to_out(out + (int64_t)u * HD + rank * slice + tid, a * inv_all);
+      for (int r = 0; r < split; ++r) a = fmaf(xo[r * slice + min(tid, slice - 1)], __shfl_sync(0xffffffffu, fr, r), a);
+      if (tid < slice) to_out(out + (int64_t)u * HD + rank * slice + tid, a * inv_all);
     }
   } else {
-    if (tid < G) {
-      float fr[Q4_SPLIT];
-      join(tid, fr);
-#pragma unroll
-      for (int r = 0; r < Q4_SPLIT; ++r) fr_s[r][tid] = fr[r];
-      all_m[tid] = m_all;
-      all_inv[tid] = inv_all;
+    if (wid < G) {
+      if (lane < split) fr_s[lane][wid] = fr;
+      if (lane == 0) { all_m[wid] = m_all; all_inv[wid] = inv_all; }
     }
     __syncthreads();
     for (int i = tid; i < G * slice; i += Q4_THREADS) {
       const int h = i >> slice_log2, ch = i & (slice - 1);
       float a = 0.f;
-#pragma unroll
-      for (int r = 0; r < Q4_SPLIT; ++r)
-        if (r < split) a = fmaf(xo[(r * G + h) * slice + ch], fr_s[r][h], a);
+      for (int r = 0; r < split; ++r) a = fmaf(xo[(r * G + h) * slice + ch], fr_s[r][h], a);
       to_out(out + ((int64_t)u * G + h) * HD + rank * slice + ch, a * all_inv[h]);
     }
   }
@@ -917,7 +931,7 @@ decode_q4_kernel(int G_arg, int split, int chunk, int depth, int B, int cap, int
           p = 0.f;
 #pragma unroll
           for (int h = 0; h < GT; ++h)
-            if (h < G) p = fmaf(exp2_fast(logit_s[h * chunk + i] - all_m[h]), all_inv[h], p);
+            if (h < G) p = fmaf(exp2_fast(logit_s[h * ld + i] - all_m[h]), all_inv[h], p);
           p /= (float)G;
         }
         const bool is_new = i == fs_local;
@@ -1000,11 +1014,19 @@ cudaError_t launch_gt(int units, int G, int B, int F, int R, int window, int nor
   auto chunk_of = [&](int split) { return ((cap + split - 1) / split + Q4_ROWS - 1) / Q4_ROWS * Q4_ROWS; };
   // a ring takes the warp's partial output in the end
   const int least = (G * HD * 4 + ITEM - 1) / ITEM > 2 ? (G * HD * 4 + ITEM - 1) / ITEM : 2;
-  auto bytes = [&](int split, int depth) { return (size_t)Q4_WARPS * depth * ITEM + (size_t)G * HD * 4 + (size_t)G * chunk_of(split) * 4; };
+  auto bytes = [&](int split, int depth) { return (size_t)Q4_WARPS * depth * ITEM + (size_t)G * HD * 4 + (size_t)G * (chunk_of(split) + 2 * Q4_EXTRA) * 4; };
   int split = 1;
   while (split < Q4_SPLIT && units * split * 2 <= Q4_FILL * sms && cap / (split * 2) >= 2 * Q4_ROWS) split *= 2;
   while (split < Q4_SPLIT && bytes(split, least) > whole_sm) split *= 2;
-  const int chunk = chunk_of(split), per_warp = (chunk / Q4_ROWS + Q4_WARPS - 1) / Q4_WARPS;
+  int chunk = chunk_of(split), ld = chunk;
+  // A few slots more than whole rounds of the warps (the incoming token's, where the budget fills them): the ninth warp of the last
+  // CTA takes them.
+  const int rounds = (B + 1) / (Q4_WARPS * Q4_ROWS * split), extra = B + 1 - rounds * Q4_WARPS * Q4_ROWS * split;
+  if (rounds > 0 && extra > 0 && extra <= Q4_EXTRA && rounds * Q4_WARPS * Q4_ROWS <= chunk) {
+    chunk = rounds * Q4_WARPS * Q4_ROWS;
+    ld = chunk + 2 * Q4_EXTRA;           // (the capacity is the slots' number rounded up to eight)
+  }
+  const int per_warp = (chunk / Q4_ROWS + Q4_WARPS - 1) / Q4_WARPS;
   int depth = 2 * per_warp;
   depth = depth < least ? least : depth > Q4_DEPTH ? Q4_DEPTH : depth;
   const size_t limit = bytes(split, least) <= half_sm ? half_sm : whole_sm;
@@ -1013,6 +1035,8 @@ cudaError_t launch_gt(int units, int G, int B, int F, int R, int window, int nor
   if (dyn > whole_sm || (int64_t)units * split > 0x7fffffffll) return cudaErrorNotSupported;
   auto kern = window > 0 ? decode_q4_kernel<T, HD, true, GT> : decode_q4_kernel<T, HD, false, GT>;
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)whole_sm);
+  if (e != cudaSuccess) return e;
+  if (split > 8) e = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(units * split));
@@ -1028,7 +1052,7 @@ cudaError_t launch_gt(int units, int G, int B, int F, int R, int window, int nor
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, kern, G, split, chunk, depth, B, cap, F, R, window, norm, scale * Q4_LOG2E, c, (const T*)q, (const T*)k,
+  return cudaLaunchKernelEx(&cfg, kern, G, split, chunk, ld, depth, B, cap, F, R, window, norm, scale * Q4_LOG2E, c, (const T*)q, (const T*)k,
                             (const T*)v, (T*)out, evicted, dev_status);
 }
 
