@@ -7,20 +7,23 @@
 // The sums over codes run on the warp-level tensor-core path (mma.sync m16n8k16, fp16 in, fp32 accumulate), the rest in fp32:
 //   * a code in the low bits of a 16-bit word IS the fp16 number code * 2^-24 (subnormal), one in bits 4-7 is code * 2^-20: unpacking
 //     is one AND per two codes and one shift per eight; the constant factors go into the other operand and the result;
-//   * that operand is exact to 2^-22 whatever its magnitude: q is scaled by a power of two per head, p_i sc_ig by one per warp and
-//     head that the largest of them determines, and both are taken as a high fp16 half and a remainder (q of bf16 inputs has none);
+//   * the other operand's magnitude does not matter: q is scaled by a power of two per head, p_i sc_ig by one per warp and head that
+//     the largest of them determines.  bf16 inputs: q is exact in fp16, p_i sc_ig is rounded to its 11 bits (2^-12 of a term, an
+//     eighth of what the output's own rounding may be off by); fp32 inputs: both as a high half and a remainder, 2^-22;
 //   * rows are stored so that the 16 bytes a lane loads hold the channels it needs in an MMA operand, of every group: rows go from
 //     global memory into operand registers by plain 8- and 16-byte loads, without shared memory.
-// A unit is split over a thread-block cluster; the slots of a CTA over eight warps, sixteen (a tile) at a time.
-//   * A tile of K or of V is 16 consecutive rows, two bulk copies (codes, parameters) into the warp's ring in shared memory.  As many
+// A unit is split over a thread-block cluster; the slots of a CTA over eight or sixteen warps, 32 at a time.
+//   * An item of K or of V is 32 consecutive rows, two bulk copies (codes, parameters) into the warp's ring in shared memory.  As many
 //     as the ring holds are requested before the launch ahead has finished; the one row that it may have appended since (last_slot) is
 //     patched in.
 //   * A warp keeps its own softmax: its maximum, sum and partial output, without a barrier between the two products.
-//   * A ninth warp takes the incoming token, which is no part of any tile: it quantises and stores the rows and is a ninth partial.
+//   * One more warp takes the incoming token, which is no part of any item: it quantises and stores the rows and is a partial of its own.
 //   * The CTA joins its partials, the cluster those of its CTAs by st.async into the partners' shared memory; every CTA then updates the
 //     indicators of its own slots, and every warp sends its eviction candidate to rank 0.
 #include <cooperative_groups.h>
 #include <cuda_fp16.h>
+
+#include <atomic>
 
 #include "q4.cuh"
 
@@ -29,13 +32,11 @@ namespace cg = cooperative_groups;
 namespace vatp {
 namespace {
 
-constexpr int Q4_WARPS = 8;            // that take slots
-constexpr int Q4_WORKERS = Q4_WARPS * 32, Q4_THREADS = Q4_WORKERS + 32;
 constexpr int Q4_TILE = 16;            // slots of an MMA tile
 constexpr int Q4_ROWS = 32;            // slots of a warp at a time: an item of its ring
 constexpr int Q4_SPLIT = 16;           // CTAs of a unit at most
 constexpr int Q4_HEADS = 8;            // query heads of a unit at most (columns of the MMA tiles)
-constexpr int Q4_EXTRA = 8;            // slots beyond the tiles that the ninth warp takes at most
+constexpr int Q4_EXTRA = 8;            // slots beyond the tiles that the last warp takes at most
 constexpr int Q4_DEPTH = 8;            // items in a warp's ring at most
 constexpr int Q4_FLUSH = 64 * Q4_ROWS;      // 255 * 15 * 257 * 2048 < 2^31
 constexpr float Q4_LOG2E = 1.4426950408889634f;
@@ -184,20 +185,21 @@ __device__ __forceinline__ unsigned long long min_key(unsigned long long key) {
 
 // GT: 1 - one query head per cache; 4 - two to four, the columns of the second product are the heads' high halves and then the
 // remainders; 8 - five to eight, a column a head and two products.
-// Dynamic shared memory: rings [8][depth][tile], which take the warps' partial outputs in the end | the ninth partial [G][HD] |
+// Dynamic shared memory: rings [WARPS][depth][item], which take the warps' partial outputs in the end | the last partial [G][HD] |
 // logits [G][ld].
 template <int HD> constexpr int q4_item = Q4_ROWS * (HD / 2 + HD / 8);      // bytes of an item: codes, then parameters
 
-template <typename T, int HD, bool WINDOWED, int GT>
-__global__ void __launch_bounds__(Q4_THREADS, 2)
+template <typename T, int HD, bool WINDOWED, int GT, int WARPS>
+__global__ void __launch_bounds__(WARPS * 32 + 32, WARPS == 8 ? 2 : 1)
 decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int cap, int F, int R, int w, int norm, float scale_log2, vatp_cache_q4 c, const T* q_new,
                  const T* k_new, const T* v_new, T* out, int32_t* evicted, int32_t* dev_status) {
+  constexpr int WORKERS = WARPS * 32, THREADS = WORKERS + 32;   // warps that take slots, and one more
   constexpr int NG = HD / 32, KW = HD / 32, VW = HD / 64;       // groups of a row; 32-bit words of a lane in a K row and a V row
   constexpr bool INT = GT == 1;                                 // products in integers (see the top)
   constexpr int KP = INT ? NG / 2 : NG;                         // parameter words of a lane per K row
   constexpr int CODES = HD / 2, PARAMS = NG * 4, ITEM = q4_item<HD>;      // bytes of a row's codes and parameters, of an item
-  constexpr bool SPLIT_Q = sizeof(T) == 4;                      // q has a remainder beyond its high half
-  constexpr int XC = GT > 4 ? 16 : 8;                           // columns of the second product's operand: see x_col
+  constexpr bool SPLIT = sizeof(T) == 4;                        // q and p sc have remainders beyond their high halves
+  constexpr int XC = GT > 4 && SPLIT ? 16 : 8;                  // columns of the second product's operand: see x_col
   constexpr int N = GT > 4 ? 1 : 2;                             // tiles a warp works on at a time (with eight heads: registers)
   constexpr int PG = N == 2 ? NG : VW;                          // groups of a lane where p sc is formed: a slot or half of one
   constexpr int XS = INT ? NG * 4 * 2 * Q4_TILE : N * NG * XC * Q4_TILE * 2;      // bytes of a warp's second operand
@@ -206,17 +208,17 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
   auto x_col = [](int h, int low) { return GT > 4 ? h + 8 * low : 2 * h + low; };
   extern __shared__ __align__(128) unsigned char dyn[];
   const int ring_bytes = depth * ITEM;                          // of a warp
-  float* new_o = reinterpret_cast<float*>(dyn + Q4_WARPS * ring_bytes);
+  float* new_o = reinterpret_cast<float*>(dyn + WARPS * ring_bytes);
   float* logit_s = new_o + G * HD;
   // the second product's operand, [tile][group][column][slot] of fp16 or [group][digit][tile][slot] of bytes; slot s of a tile
   // stands at 4 (s mod 4) + s / 4
-  __shared__ __align__(16) unsigned char xs[Q4_WARPS][XS];
-  __shared__ float part_m[Q4_WARPS + 1][GT], part_l[Q4_WARPS + 1][GT], part_lo[Q4_WARPS][GT][NG];
+  __shared__ __align__(16) unsigned char xs[WARPS][XS];
+  __shared__ float part_m[WARPS + 1][GT], part_l[WARPS + 1][GT], part_lo[WARPS][GT][NG];
   __shared__ float xo[GT * HD];                                         // slices of partial outputs received [split][G][HD / split]
   __shared__ float2 ex_ml[Q4_SPLIT][GT];                                // per rank and head: maximum of its logits, sum of exp2(s - m)
   __shared__ float fr_s[Q4_SPLIT][GT], all_m[GT], all_inv[GT], new_norm_s;
-  __shared__ Q4Candidate cand[Q4_SPLIT * Q4_WARPS];                     // in rank 0
-  __shared__ __align__(8) uint64_t full[Q4_WARPS][Q4_DEPTH], k_done, ex_bar, cand_bar;
+  __shared__ Q4Candidate cand[Q4_SPLIT * WARPS];                     // in rank 0
+  __shared__ __align__(8) uint64_t full[WARPS][Q4_DEPTH], k_done, ex_bar, cand_bar;
 
   const int rank = split > 1 ? (int)cg::this_cluster().block_rank() : 0;
   const int tid = threadIdx.x, lane = tid & 31, wid = __shfl_sync(0xffffffffu, tid >> 5, 0);
@@ -225,18 +227,18 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
   // this CTA's slots of the unit: those of the tiles, and in the last CTA up to Q4_EXTRA more (see launch_gt)
   const int s0 = min(rank * chunk, cap), rows_alloc = min(chunk, cap - s0), rows_all = rank == split - 1 ? cap - s0 : rows_alloc;
   const int64_t base = (int64_t)u * cap + s0;
-  if (tid < Q4_WARPS * Q4_DEPTH) bar_init(&full[0][tid], 1);
-  if (tid == Q4_WORKERS) {
-    bar_init(&k_done, Q4_WARPS + 1);
+  if (tid < WARPS * Q4_DEPTH) bar_init(&full[0][tid], 1);
+  if (tid == WORKERS) {
+    bar_init(&k_done, WARPS + 1);
     bar_init(&ex_bar, 1);
     bar_init(&cand_bar, 1);
   }
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-  if (tid == Q4_WORKERS) {
+  if (tid == WORKERS) {
     bar_expect(s32(&ex_bar), (uint32_t)(8 * G * split + 4 * G * HD));
-    if (rank == 0) bar_expect(s32(&cand_bar), (uint32_t)(split * Q4_WARPS * sizeof(Q4Candidate)));
+    if (rank == 0) bar_expect(s32(&cand_bar), (uint32_t)(split * WARPS * sizeof(Q4Candidate)));
   }
-  if (!INT && wid < Q4_WARPS)      // (columns without a head stay 0)
+  if (!INT && wid < WARPS)      // (columns without a head stay 0)
     for (int i = lane; i < XS / 4; i += 32) reinterpret_cast<uint32_t*>(xs[wid])[i] = 0u;
   __syncthreads();
   // Another CTA's shared memory may only be written once that CTA runs and its barriers are armed: everyone arrives here and
@@ -249,11 +251,11 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
   const unsigned char* kp = static_cast<const unsigned char*>(c.k_params) + base * PARAMS;
   const unsigned char* vp = static_cast<const unsigned char*>(c.v_params) + base * PARAMS;
   unsigned char* ring = dyn + (size_t)wid * ring_bytes;
-  // This warp's items: rows 32 (wid + 8 j) ..; n of them among the first `rows` slots.  Item j < n of its ring holds rows of K, item
+  // This warp's items: rows 32 (wid + WARPS j) ..; n of them among the first `rows` slots.  Item j < n of its ring holds rows of K, item
   // n + j of V.
-  auto items_in = [&](int rows) { return max(rows - wid * Q4_ROWS + Q4_WARPS * Q4_ROWS - 1, 0) / (Q4_WARPS * Q4_ROWS); };
-  auto item_row = [&](int j) { return (wid + Q4_WARPS * j) * Q4_ROWS; };
-  const uint32_t ring_a = s32(ring), full_a = s32(&full[wid < Q4_WARPS ? wid : 0][0]);
+  auto items_in = [&](int rows) { return max(rows - wid * Q4_ROWS + WARPS * Q4_ROWS - 1, 0) / (WARPS * Q4_ROWS); };
+  auto item_row = [&](int j) { return (wid + WARPS * j) * Q4_ROWS; };
+  const uint32_t ring_a = s32(ring), full_a = s32(&full[wid < WARPS ? wid : 0][0]);
   auto request = [&](int j, int n, int slot) {      // one lane: item j into ring slot `slot`
     const bool is_v = j >= n;
     const unsigned r0 = item_row(is_v ? j - n : j), rows = min(Q4_ROWS, rows_alloc - (int)r0);      // (a multiple of eight)
@@ -262,7 +264,7 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
     bulk_load(dst, (is_v ? vc : kc) + (uint64_t)r0 * CODES, rows * CODES, bar);
     bulk_load(dst + Q4_ROWS * CODES, (is_v ? vp : kp) + (uint64_t)r0 * PARAMS, rows * PARAMS, bar);
   };
-  const int n_alloc = wid < Q4_WARPS ? items_in(rows_alloc) : 0, early = min(depth, 2 * n_alloc);
+  const int n_alloc = wid < WARPS ? items_in(rows_alloc) : 0, early = min(depth, 2 * n_alloc);
   if (lane == 0)
     for (int j = 0; j < early; ++j) request(j, n_alloc, j);
   __syncwarp();
@@ -271,8 +273,8 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int len_m = c.state.len[u], fs_m = c.state.free_slot[u], t = c.state.next_pos[u], ls = c.state.last_slot[u];
 
-  if (wid == Q4_WARPS) {
-    // ---- the ninth warp: the incoming token.  Lane l < HD / 4 has channels 4 l .. 4 l + 3.
+  if (wid == WARPS) {
+    // ---- the last warp: the incoming token.  Lane l < HD / 4 has channels 4 l .. 4 l + 3.
     float kv[2][4], qv[GT][4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -359,7 +361,7 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
     if (lane == 0) {
 #pragma unroll
       for (int h = 0; h < GT; ++h)
-        if (GT == 1 || h < G) part_m[Q4_WARPS][h] = m[h];
+        if (GT == 1 || h < G) part_m[WARPS][h] = m[h];
       bar_arrive(s32(&k_done));
     }
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -369,9 +371,9 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
       if (GT > 1 && h >= G) continue;
       float top = m[h];
 #pragma unroll
-      for (int k = 0; k < Q4_WARPS; ++k) top = fmaxf(top, part_m[k][h]);
+      for (int k = 0; k < WARPS; ++k) top = fmaxf(top, part_m[k][h]);
       const float f = m[h] > -INFINITY ? exp2_fast(m[h] - top) : 0.f;
-      if (lane == 0) part_l[Q4_WARPS][h] = l[h] * f;
+      if (lane == 0) part_l[WARPS][h] = l[h] * f;
       if (lane < HD / 4) *reinterpret_cast<float4*>(new_o + h * HD + 4 * lane) = make_float4(o[h][0] * f, o[h][1] * f, o[h][2] * f, o[h][3] * f);
     }
   }
@@ -388,7 +390,7 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
   auto fetch = [&](int i0) {
 #pragma unroll
     for (int k = 0; k < SB; ++k) {
-      const int i = i0 + k * Q4_WORKERS;
+      const int i = i0 + k * WORKERS;
       old_r[k] = norm_r[k] = 0.f;
       pos_r[k] = 0;
       if (WINDOWED) fx_r[k] = 0;
@@ -401,10 +403,10 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
     }
   };
 
-  if (wid < Q4_WARPS) {
+  if (wid < WARPS) {
     // ---- B operand of K q^T.  Lane (n = r8, t4): channels 8 t4 .. 8 t4 + 7 of groups of its column.
     // INT: columns 0 - 3 are the four digits of group 0 (then of group 2), columns 4 - 7 of group 1 (3).  Else: column n is head n.
-    uint32_t qb[NG][INT ? 2 : 4], qr[GT > 1 && SPLIT_Q ? NG : 1][4];
+    uint32_t qb[NG][INT ? 2 : 4], qr[GT > 1 && SPLIT ? NG : 1][4];
     // what a sum is to be multiplied by (INT: of the lane's two digits); sums of q over groups, * scale
     float q_back[2], qsum[INT ? NG / 2 : NG][2];
     {
@@ -467,7 +469,7 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
             const float f = x & 1 ? up * 0.0625f : up, p0 = q[g][x] * f, p1 = q[g][x + 4] * f;      // (odd channels' codes stand four bits higher)
             const __half2 h = __floats2half2_rn(p0, p1);
             qb[g][x] = *reinterpret_cast<const uint32_t*>(&h);
-            if constexpr (SPLIT_Q) qr[g][x] = half2_of(p0 - __low2float(h), p1 - __high2float(h));
+            if constexpr (SPLIT) qr[g][x] = half2_of(p0 - __low2float(h), p1 - __high2float(h));
           }
         // (an accumulator's columns are heads 2 t4 and 2 t4 + 1; their sums are with the lanes of those columns)
 #pragma unroll
@@ -503,8 +505,8 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
       if (lane == 0 && !bad)
         for (int j = 0; j < next; ++j) request(j, n, (slot + j) % depth);
       __syncwarp();
-    } else if (ls >= 0 && ls != fs && ls_local >= 0 && ls_local < cnt_t && ls_local / Q4_ROWS % Q4_WARPS == wid) {
-      ls_item = ls_local / (Q4_ROWS * Q4_WARPS);
+    } else if (ls >= 0 && ls != fs && ls_local >= 0 && ls_local < cnt_t && ls_local / Q4_ROWS % WARPS == wid) {
+      ls_item = ls_local / (Q4_ROWS * WARPS);
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
         if (lane < CODES / 4) ls_word[x] = load_fresh(reinterpret_cast<const uint32_t*>((x ? vc : kc) + (int64_t)ls_local * CODES) + lane);
@@ -575,7 +577,7 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
         b += __shfl_xor_sync(0xffffffffu, odd ? s[2] : s[3], 1);
         float x = (up ? b : a) + __shfl_xor_sync(0xffffffffu, up ? a : b, 2);
         const int row = r0 + r8 + 8 * t4;
-        if (row >= cnt_t || row == fs_local) x = -INFINITY;      // (the incoming token's slot is the ninth warp's)
+        if (row >= cnt_t || row == fs_local) x = -INFINITY;      // (the incoming token's slot is the last warp's)
         if (row < cnt_t && row != fs_local) logit_s[row] = x;
         m_run[0] = fmaxf(m_run[0], x);
       } else {
@@ -591,7 +593,7 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
             d[0] = d[1] = d[2] = d[3] = 0.f;
             mma_f16(d, xa & 0x000f000fu, xb & 0x000f000fu, xa & 0x00f000f0u, xb & 0x00f000f0u, qb[g][0], qb[g][1]);
             mma_f16(d, ya & 0x000f000fu, yb & 0x000f000fu, ya & 0x00f000f0u, yb & 0x00f000f0u, qb[g][2], qb[g][3]);
-            if constexpr (SPLIT_Q) {
+            if constexpr (SPLIT) {
               mma_f16(d, xa & 0x000f000fu, xb & 0x000f000fu, xa & 0x00f000f0u, xb & 0x00f000f0u, qr[g][0], qr[g][1]);
               mma_f16(d, ya & 0x000f000fu, yb & 0x000f000fu, ya & 0x00f000f0u, yb & 0x00f000f0u, qr[g][2], qr[g][3]);
             }
@@ -737,18 +739,25 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
           l_run[h] += p;
 #pragma unroll
           for (int i = 0; i < PG; ++i) {
-            const float x = y * q4_scale(pr[i]);
             lo_run[h][i] = fmaf(p, q4_low(pr[i]), lo_run[h][i]);
             if constexpr (INT) {             // a column for each byte
-              const uint32_t X = __float2uint_rn(x);
+              const uint32_t X = __float2uint_rn(y * q4_scale(pr[i]));
               unsigned char* to = xs[wid] + (my_group + i) * 4 * 2 * Q4_TILE + x_at;
 #pragma unroll
               for (int d = 0; d < 4; ++d) to[d * 2 * Q4_TILE] = (unsigned char)(X >> (8 * d));
-            } else {
-              const __half hh = __float2half_rn(x), hl = __float2half_rn(x - __half2float(hh));
+            } else if ((i & 1) == 0) {
+              const int i1 = PG > 1 ? i + 1 : i;
+              const float x0 = y * q4_scale(pr[i]), x1 = y * q4_scale(pr[i1]);
+              const __half2 hh = __floats2half2_rn(x0, x1);
               uint16_t* to = reinterpret_cast<uint16_t*>(xs[wid]) + ((my_group + i) * XC + x_col(h, 0)) * Q4_TILE + x_at;
-              to[0] = __half_as_ushort(hh);
-              to[(x_col(h, 1) - x_col(h, 0)) * Q4_TILE] = __half_as_ushort(hl);
+              to[0] = __half_as_ushort(__low2half(hh));
+              if (PG > 1) to[XC * Q4_TILE] = __half_as_ushort(__high2half(hh));
+              if constexpr (SPLIT) {
+                const __half2 hl = __floats2half2_rn(x0 - __low2float(hh), x1 - __high2float(hh));
+                to += (x_col(h, 1) - x_col(h, 0)) * Q4_TILE;
+                to[0] = __half_as_ushort(__low2half(hl));
+                if (PG > 1) to[XC * Q4_TILE] = __half_as_ushort(__high2half(hl));
+              }
             }
           }
         }
@@ -789,7 +798,7 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
             const uint32_t ya = xa >> 8, yb = xb >> 8;
             mma_f16(o_acc[g][0], xa & 0x000f000fu, xa & 0x00f000f0u, xb & 0x000f000fu, xb & 0x00f000f0u, b.x, b.y);
             mma_f16(o_acc[g][1], ya & 0x000f000fu, ya & 0x00f000f0u, yb & 0x000f000fu, yb & 0x00f000f0u, b.x, b.y);
-            if constexpr (GT > 4) {
+            if constexpr (GT > 4 && SPLIT) {
               const uint2 d = *reinterpret_cast<const uint2*>(xh + 8 * Q4_TILE);
               mma_f16(o_acc[g][0], xa & 0x000f000fu, xa & 0x00f000f0u, xb & 0x000f000fu, xb & 0x00f000f0u, d.x, d.y);
               mma_f16(o_acc[g][1], ya & 0x000f000fu, ya & 0x00f000f0u, yb & 0x000f000fu, yb & 0x00f000f0u, d.x, d.y);
@@ -819,7 +828,7 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
       if (GT == 1 || h < G) {
         float m = m_own[h];
 #pragma unroll
-        for (int k = 0; k <= Q4_WARPS; ++k) m = fmaxf(m, part_m[k][h]);
+        for (int k = 0; k <= WARPS; ++k) m = fmaxf(m, part_m[k][h]);
         const bool any = m_own[h] > -INFINITY;
         const float fm = any ? exp2_fast(m_own[h] - m) : 0.f, fj = any ? exp2_fast((float)(J[h] - 126 - X_TOP + (INT ? 0 : 24)) - m) : 0.f;
 #pragma unroll
@@ -865,19 +874,19 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
   const int slice = HD / split, slice_log2 = 31 - __clz(slice);
   if (tid < split * G) {
     const int h = tid / split, dst = tid - h * split;
-    float m = part_m[Q4_WARPS][h], l = part_l[Q4_WARPS][h];
+    float m = part_m[WARPS][h], l = part_l[WARPS][h];
 #pragma unroll
-    for (int k = 0; k < Q4_WARPS; ++k) {
+    for (int k = 0; k < WARPS; ++k) {
       m = fmaxf(m, part_m[k][h]);
       l += part_l[k][h];
     }
     send2(at_rank(s32(&ex_ml[rank][h]), dst), m, l, at_rank(s32(&ex_bar), dst));
   }
-  for (int i = tid; i < G * HD; i += Q4_THREADS) {
+  for (int i = tid; i < G * HD; i += THREADS) {
     const int h = i / HD, ch = i - h * HD;
     float a = new_o[i];
 #pragma unroll
-    for (int k = 0; k < Q4_WARPS; ++k) a += reinterpret_cast<const float*>(dyn + (size_t)k * ring_bytes)[i] + part_lo[k][h][ch >> 5];
+    for (int k = 0; k < WARPS; ++k) a += reinterpret_cast<const float*>(dyn + (size_t)k * ring_bytes)[i] + part_lo[k][h][ch >> 5];
     const int dst = ch >> slice_log2;
     send(at_rank(s32(&xo[(rank * G + h) * slice + (ch & (slice - 1))]), dst), a, at_rank(s32(&ex_bar), dst));
   }
@@ -906,7 +915,7 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
       if (lane == 0) { all_m[wid] = m_all; all_inv[wid] = inv_all; }
     }
     __syncthreads();
-    for (int i = tid; i < G * slice; i += Q4_THREADS) {
+    for (int i = tid; i < G * slice; i += THREADS) {
       const int h = i >> slice_log2, ch = i & (slice - 1);
       float a = 0.f;
       for (int r = 0; r < split; ++r) a = fmaf(xo[(r * G + h) * slice + ch], fr_s[r][h], a);
@@ -916,13 +925,13 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
 
   // ---- indicator update (Eq. 2 / Eq. 3) and importance (Eq. 4) of this CTA's slots, every warp's arg-min to rank 0
   const bool evicting = hi > B;
-  if (wid < Q4_WARPS) {
+  if (wid < WARPS) {
     unsigned long long my_key = Q4_NO_KEY;
     int my_slot = -1, my_pos = -1;
     for (int i0 = tid; i0 < cnt;) {
 #pragma unroll
       for (int k = 0; k < SB; ++k) {
-        const int i = i0 + k * Q4_WORKERS;
+        const int i = i0 + k * WORKERS;
         if (i >= cnt) continue;
         float p;
         if constexpr (GT == 1) {
@@ -952,19 +961,19 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
           if (key < my_key) { my_key = key; my_slot = s0 + i; my_pos = ps; }
         }
       }
-      i0 += SB * Q4_WORKERS;
+      i0 += SB * WORKERS;
       if (i0 < cnt) fetch(i0);
     }
     if (WINDOWED) {
       // recycled slot: the other rows of its ring column belong to the previous occupant (shared out over the unit's CTAs)
-      for (int r = rank * Q4_WORKERS + tid; r < w; r += split * Q4_WORKERS)
+      for (int r = rank * WORKERS + tid; r < w; r += split * WORKERS)
         if (r != t % w) c.state.ring[((int64_t)u * w + r) * cap + fs] = 0.f;
     }
     if (evicting) {
       // (positions are unique: one lane holds the winning key)
       const unsigned long long win = min_key(my_key);
       if (win == Q4_NO_KEY ? lane == 0 : my_key == win)
-        send4(at_rank(s32(&cand[rank * Q4_WARPS + wid]), 0), (uint32_t)win, (uint32_t)(win >> 32), (uint32_t)my_slot, (uint32_t)my_pos, at_rank(s32(&cand_bar), 0));
+        send4(at_rank(s32(&cand[rank * WARPS + wid]), 0), (uint32_t)win, (uint32_t)(win >> 32), (uint32_t)my_slot, (uint32_t)my_pos, at_rank(s32(&cand_bar), 0));
     }
   } else if (rank == 0) {
     int out_slot = hi, left = hi, ev = -1;                         // not evicting: the cache grows
@@ -972,7 +981,7 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
     if (evicting) {
       if (!bar_wait(s32(&cand_bar), 0)) bad = true;
       Q4Candidate best{Q4_NO_KEY, -1, -1};
-      for (int i = lane; i < split * Q4_WARPS; i += 32)
+      for (int i = lane; i < split * WARPS; i += 32)
         if (cand[i].key < best.key) best = cand[i];
       const unsigned long long win = min_key(best.key);
       if (win != Q4_NO_KEY) {
@@ -1001,46 +1010,86 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
   }
 }
 
-#ifndef Q4_FILL
-#define Q4_FILL 1
-#endif
+// How many clusters of `split` CTAs with an SM each run at once (they lie within a GPC, which is not a multiple of them); looked up
+// once per device and size.
+template <typename Kernel>
+int clusters_at_once(Kernel kern, int split, int threads, size_t dyn) {
+  static std::atomic<int> known[16][5];
+  int dev = 0, log2 = 31 - __builtin_clz(split);
+  if (cudaGetDevice(&dev) != cudaSuccess) return 0;
+  std::atomic<int>* entry = dev < 16 ? &known[dev][log2] : nullptr;
+  if (entry && entry->load()) return entry->load() - 1;
+  if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)dyn) != cudaSuccess ||
+      cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) {
+    cudaGetLastError();
+    return 0;
+  }
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)split);
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = dyn;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = split;
+  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  int n = 0;
+  if (cudaOccupancyMaxActiveClusters(&n, kern, &cfg) != cudaSuccess) { cudaGetLastError(); n = 0; }
+  if (entry) entry->store(n + 1);
+  return n;
+}
+
 template <typename T, int HD, int GT>
 cudaError_t launch_gt(int units, int G, int B, int F, int R, int window, int norm, float scale, const vatp_cache_q4& c, const void* q,
                       const void* k, const void* v, void* out, int32_t* evicted, int32_t* dev_status, cudaStream_t st) {
   const int cap = cache_capacity(B), sms = device_sm_count();
   constexpr int ITEM = q4_item<HD>;
-  // Static arrays and what the system takes, rounded up; half of an SM's shared memory and all of it.
-  constexpr size_t fixed = (GT > 4 ? 27 : GT > 1 ? 23 : 9) * 1024, half_sm = 113 * 1024 - fixed, whole_sm = 226 * 1024 - fixed;
-  auto chunk_of = [&](int split) { return ((cap + split - 1) / split + Q4_ROWS - 1) / Q4_ROWS * Q4_ROWS; };
+  // Static arrays and what the system takes, rounded up (of a CTA of sixteen warps, of one of eight).
+  constexpr size_t fixed16 = (GT > 4 ? 48 : GT > 1 ? 42 : 18) * 1024, fixed8 = (GT > 4 ? 29 : GT > 1 ? 25 : 11) * 1024;
+  const bool win = window > 0;
+  auto kern16 = win ? decode_q4_kernel<T, HD, true, GT, 16> : decode_q4_kernel<T, HD, false, GT, 16>;
+  auto kern8 = win ? decode_q4_kernel<T, HD, true, GT, 8> : decode_q4_kernel<T, HD, false, GT, 8>;
+  const size_t most16 = 226 * 1024 - fixed16, most8 = 226 * 1024 - fixed8;
+  // Units on fewer CTAs than SMs: an SM to a CTA (two of a launch on one SM while others idle: 32 units x 2049 slots, four CTAs each,
+  // 8.0 and 7.3 us per step), as many CTAs per unit as run at once and find some slots, of sixteen warps when there are more than
+  // three rounds for eight (74 units x 4097: 15.7 and 14.0 us; 32 x 1025: 6.0 and 6.8, which is why not always).  More units
+  // than SMs: one CTA of eight warps each, two on an SM.
+  int split = 1;
+  while (split < Q4_SPLIT && units * split * 2 <= sms && cap / split >= 4 * Q4_ROWS && clusters_at_once(kern16, split * 2, 17 * 32, most16) >= units) split *= 2;
+  const bool alone = units <= sms;
   // a ring takes the warp's partial output in the end
   const int least = (G * HD * 4 + ITEM - 1) / ITEM > 2 ? (G * HD * 4 + ITEM - 1) / ITEM : 2;
-  auto bytes = [&](int split, int depth) { return (size_t)Q4_WARPS * depth * ITEM + (size_t)G * HD * 4 + (size_t)G * (chunk_of(split) + 2 * Q4_EXTRA) * 4; };
-  int split = 1;
-  while (split < Q4_SPLIT && units * split * 2 <= Q4_FILL * sms && cap / (split * 2) >= 2 * Q4_ROWS) split *= 2;
-  while (split < Q4_SPLIT && bytes(split, least) > whole_sm) split *= 2;
+  auto chunk_of = [&](int split) { return ((cap + split - 1) / split + Q4_ROWS - 1) / Q4_ROWS * Q4_ROWS; };
+  int warps = 8;
+  auto bytes = [&](int split, int depth) { return (size_t)warps * depth * ITEM + (size_t)G * HD * 4 + (size_t)G * (chunk_of(split) + 2 * Q4_EXTRA) * 4; };
+  const size_t half = 113 * 1024 - fixed8;
+  if (alone ? (cap + split - 1) / split > 3 * 8 * Q4_ROWS : bytes(split, least) > half) warps = 16;      // (half: two CTAs on an SM)
+  const size_t most = warps == 16 ? most16 : most8;
+  while (split < Q4_SPLIT && bytes(split, least) > most) split *= 2;      // (the logits of a CTA's slots stand in shared memory)
   int chunk = chunk_of(split), ld = chunk;
-  // A few slots more than whole rounds of the warps (the incoming token's, where the budget fills them): the ninth warp of the last
+  // A few slots more than whole rounds of the warps (the incoming token's, where the budget fills them): the last warp of the last
   // CTA takes them.
-  const int rounds = (B + 1) / (Q4_WARPS * Q4_ROWS * split), extra = B + 1 - rounds * Q4_WARPS * Q4_ROWS * split;
-  if (rounds > 0 && extra > 0 && extra <= Q4_EXTRA && rounds * Q4_WARPS * Q4_ROWS <= chunk) {
-    chunk = rounds * Q4_WARPS * Q4_ROWS;
+  const int round = warps * Q4_ROWS * split, rounds = (B + 1) / round, extra = B + 1 - rounds * round;
+  if (rounds > 0 && extra > 0 && extra <= Q4_EXTRA && rounds * warps * Q4_ROWS <= chunk) {
+    chunk = rounds * warps * Q4_ROWS;
     ld = chunk + 2 * Q4_EXTRA;           // (the capacity is the slots' number rounded up to eight)
   }
-  const int per_warp = (chunk / Q4_ROWS + Q4_WARPS - 1) / Q4_WARPS;
+  const int per_warp = (chunk / Q4_ROWS + warps - 1) / warps;
   int depth = 2 * per_warp;
   depth = depth < least ? least : depth > Q4_DEPTH ? Q4_DEPTH : depth;
-  const size_t limit = bytes(split, least) <= half_sm ? half_sm : whole_sm;
+  const size_t limit = !alone && warps == 8 ? half : most;
   while (depth > least && bytes(split, depth) > limit) --depth;
-  const size_t dyn = bytes(split, depth);
-  if (dyn > whole_sm || (int64_t)units * split > 0x7fffffffll) return cudaErrorNotSupported;
-  auto kern = window > 0 ? decode_q4_kernel<T, HD, true, GT> : decode_q4_kernel<T, HD, false, GT>;
-  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)whole_sm);
-  if (e != cudaSuccess) return e;
-  if (split > 8) e = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+  size_t dyn = bytes(split, depth);
+  if (dyn > most || (int64_t)units * split > 0x7fffffffll) return cudaErrorNotSupported;
+  if (alone && dyn < 120 * 1024 - fixed8) dyn = 120 * 1024 - fixed8;
+  auto kern = warps == 16 ? kern16 : kern8;
+  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most);
+  if (e == cudaSuccess && split > 8) e = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(units * split));
-  cfg.blockDim = dim3(Q4_THREADS);
+  cfg.blockDim = dim3((unsigned)(warps * 32 + 32));
   cfg.dynamicSmemBytes = dyn;
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
@@ -1052,8 +1101,8 @@ cudaError_t launch_gt(int units, int G, int B, int F, int R, int window, int nor
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, kern, G, split, chunk, ld, depth, B, cap, F, R, window, norm, scale * Q4_LOG2E, c, (const T*)q, (const T*)k,
-                            (const T*)v, (T*)out, evicted, dev_status);
+  return cudaLaunchKernelEx(&cfg, kern, G, split, chunk, ld, depth, B, cap, F, R, window, norm, scale * Q4_LOG2E, c, (const T*)q,
+                            (const T*)k, (const T*)v, (T*)out, evicted, dev_status);
 }
 
 template <typename T, int HD>

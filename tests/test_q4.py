@@ -1,8 +1,7 @@
 """The decode state held in 4 bits on the GPU: compaction into it, conversion, generation steps, copies of entries.
 
 Codes, parameters and copies are exact.  Steps are held to bounds that count roundings (tests/q4_reference.py): the logits' 32-bit
-sums give a probability a relative error `rel`; the output adds 2^-20 of what its two parts amount to (p in two 16-bit halves) and
-its own rounding to 16 bits.
+sums give a probability a relative error `rel`; the output adds the roundings of its terms and its own to 16 bits.
 """
 import os
 import subprocess
@@ -212,6 +211,9 @@ def _run_steps(p, c, n_steps, dtype, *, seed=9):
     norm = {v: k for k, v in V.NORM_KINDS.items()}[p.norm_kind]
     ref = Q.State(c, d, p.budget, p.n_sink, p.n_recent, p.scale, w, norm)
     g, status, eps = _gen(seed), _status(), torch.finfo(DT[dtype]).eps / 2
+    # a term p sc code of the output: with grouped bf16 queries p sc is rounded to fp16 (half a step is 2^-12 of it), else
+    # 2^-20 covers what is left of it in two halves or in 32 bits
+    term = 2.0 ** -12 + 2.0 ** -20 if G > 1 and dtype == "bf16" else 2.0 ** -20
     p_off = torch.zeros(b * h, 1, dtype=torch.float64, device="cuda")
     for i in range(n_steps):
         q, k, v = torch.randn(b, p.heads, d, generator=g, device="cuda").to(DT[dtype]), _rows(g, b, h, d, dtype=dtype), _rows(g, b, h, d, dtype=dtype)
@@ -221,7 +223,7 @@ def _run_steps(p, c, n_steps, dtype, *, seed=9):
         assert int(status) == 0
         want, pm, I, may_go, rel, v_mag = ref.step(q.view(b * h, G, d), k.view(b * h, d), v.view(b * h, d))
         off = (out.double().view(b * h, G, d) - want).abs()
-        bound = (rel[..., None] + 2.0 ** -20) * v_mag + eps * want.abs() + 1e-30
+        bound = (rel[..., None] + term) * v_mag + eps * want.abs() + 1e-30
         assert torch.all(off <= bound), f"step {i}: out, worst {float((off / bound).max())} of the bound"
         # an indicator is what it was plus the steps' probabilities p_j, each off by rel_j p_j at most: together by
         # sum_j rel_j p_j <= (max_j rel_j) S; a step adds a rounding of the sum, and a probability below 2^-126, the smallest normal
