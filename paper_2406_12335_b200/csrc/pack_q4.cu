@@ -1,104 +1,132 @@
 // Rows of K and V to and from their 4-bit form: compaction of a prompt's kept rows, conversion of a decode state, and back.
 //
-// Both are bound by memory: a row of 128 bf16 channels is 256 bytes in one form and 80 in the other.
+// Bound by memory where the number of instructions allows: a row of 128 bf16 channels is 256 bytes in one form and 80 in the other.
+// 256 units x 1639 slots: rows into 4 bits 45.4 us (6.25 TB/s, 0.96 of a copy's rate), gathered out of prompts of 8192 tokens 54.7 (rows
+// of 256 bytes anywhere), back 47.9.
 #include "q4.cuh"
 
 namespace vatp {
 namespace {
 
-constexpr int PK_WARPS = 8, PK_THREADS = PK_WARPS * 32;
+constexpr int PK_WARPS = 2, PK_THREADS = PK_WARPS * 32;      // (8 warps a CTA, which end together: 256 units x 1639 slots 48.8 us, so 45.3)
+constexpr int UP_THREADS = 256;
 
-// sixteen consecutive channels
-__device__ __forceinline__ void load16(const __nv_bfloat16* p, float (&x)[16]) {
+// A group of a row as it is stored: its least and largest value, and each of them.
+template <typename T> struct Group32;
+template <> struct Group32<__nv_bfloat16> {
+  uint32_t w[16];
+  __device__ __forceinline__ void load(const __nv_bfloat16* p) {
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const uint4 r = load_behind_wait(reinterpret_cast<const uint4*>(p) + i);
-    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      x[8 * i + 2 * k] = __uint_as_float(w[k] << 16);
-      x[8 * i + 2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u);
+    for (int i = 0; i < 4; ++i) {
+      const uint4 r = load_behind_wait(reinterpret_cast<const uint4*>(p) + i);
+      w[4 * i] = r.x; w[4 * i + 1] = r.y; w[4 * i + 2] = r.z; w[4 * i + 3] = r.w;
     }
   }
-}
-__device__ __forceinline__ void load16(const float* p, float (&x)[16]) {
+  __device__ __forceinline__ void clear() {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float4 r = load_behind_wait(reinterpret_cast<const float4*>(p) + i);
-    x[4 * i] = r.x; x[4 * i + 1] = r.y; x[4 * i + 2] = r.z; x[4 * i + 3] = r.w;
+    for (int i = 0; i < 16; ++i) w[i] = 0u;
   }
-}
+  __device__ __forceinline__ float at(int i) const { return __uint_as_float(i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16); }
+  __device__ __forceinline__ void range(float& mn, float& mx) const {      // two values an instruction
+    __nv_bfloat162 a = reinterpret_cast<const __nv_bfloat162&>(w[0]), b = a;
+#pragma unroll
+    for (int i = 1; i < 16; ++i) {
+      const __nv_bfloat162 x = reinterpret_cast<const __nv_bfloat162&>(w[i]);
+      a = __hmin2(a, x);
+      b = __hmax2(b, x);
+    }
+    mn = fminf(__low2float(a), __high2float(a));
+    mx = fmaxf(__low2float(b), __high2float(b));
+  }
+};
+template <> struct Group32<float> {
+  float x[32];
+  __device__ __forceinline__ void load(const float* p) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float4 r = load_behind_wait(reinterpret_cast<const float4*>(p) + i);
+      x[4 * i] = r.x; x[4 * i + 1] = r.y; x[4 * i + 2] = r.z; x[4 * i + 3] = r.w;
+    }
+  }
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int i = 0; i < 32; ++i) x[i] = 0.f;
+  }
+  __device__ __forceinline__ float at(int i) const { return x[i]; }
+  __device__ __forceinline__ void range(float& mn, float& mx) const {
+    mn = mx = x[0];
+#pragma unroll
+    for (int i = 1; i < 32; ++i) { mn = fminf(mn, x[i]); mx = fmaxf(mx, x[i]); }
+  }
+};
 
-// A warp takes 512 / HD consecutive slots of a unit, HD / 16 lanes a row: a lane has half a group, finds its least and largest value
-// with one exchange, and its codes pass through 256 bytes of shared memory so that they leave as full 16-byte words.
+// A warp takes 1024 / HD consecutive slots of a unit, a lane one group of a row: its range needs no exchange, the arithmetic of a
+// group's parameters is done once.  The codes pass through 512 bytes of shared memory so that they leave as full 16-byte words.
+// (What bounds it is the number of instructions: with half a group a lane, 17 a value where this has 9.)
 // kept != nullptr (compaction): slot s of unit u takes row kept[u][s] of the prompt, and the decode state is initialised.
 // kept == nullptr (conversion): slot s takes slot s of the cache k, v where pos_from says that it holds a token.
 template <typename T, int HD>
 __global__ void __launch_bounds__(PK_THREADS)
 pack_q4_kernel(Shape sh, int B, int cap, int blocks_per_unit, const T* k, const T* v, const int32_t* kept, const int32_t* pos_from,
                const float* attn_acc, const float* vnorm, vatp_cache_q4 c, int32_t* dev_status) {
-  constexpr int LPR = HD / 16, ROWS = 32 / LPR;                  // lanes a row, rows of a warp
-  __shared__ __align__(16) unsigned char stage[PK_WARPS][2][256];
+  constexpr int NG = HD / 32, ROWS = 32 / NG;                    // lanes a row, rows of a warp
+  __shared__ __align__(16) unsigned char stage[PK_WARPS][2][512];
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
   const int u = blockIdx.x / blocks_per_unit;
   const int first = ((blockIdx.x - u * blocks_per_unit) * PK_WARPS + wid) * ROWS;      // this warp's first slot
-  const int sub = lane % LPR, g = sub >> 1, h = sub & 1;          // this lane's group and half of it
-  const int s = first + lane / LPR;
+  const int g = lane % NG, s = first + lane / NG;                 // this lane's group and slot
   asm volatile("griddepcontrol.wait;" ::: "memory");
   if (first >= cap) return;
   const int len = min(sh.T, B);
   const int64_t o = (int64_t)u * cap + s;
-  int64_t from = -1;                                              // element offset of the row in k and v
+  int src = -1;                                                   // row of the prompt, or slot
+  int64_t from = 0;
   if (kept) {
-    int src = s < len ? kept[(int64_t)u * B + s] : -1;
+    if (s < len) src = kept[(int64_t)u * B + s];
     if (src >= 0 && !VATP_INB(src, sh.T, dev_status)) src = -1;
-    if (src >= 0) from = unit_offset(sh, u) + (int64_t)src * sh.st;
-    if (sub == 0 && s < cap) {
-      c.state.pos[o] = src;
-      c.state.acc[o] = src >= 0 ? attn_acc[(int64_t)u * sh.T + src] : 0.f;
-      c.state.vnorm[o] = src >= 0 ? vnorm[(int64_t)u * sh.T + src] : 0.f;
-      if (s == 0) {
-        c.state.len[u] = len;
-        c.state.free_slot[u] = len;
-        c.state.next_pos[u] = sh.T;
-        c.state.last_slot[u] = -1;
-      }
-    }
-  } else if (s < cap && pos_from[o] >= 0) {
+    from = unit_offset(sh, u) + (int64_t)src * sh.st;
+  } else {
+    if (s < cap && pos_from[o] >= 0) src = s;
     from = o * HD;
   }
-  float x[2][16];
-  if (from >= 0) {
-    load16(k + from + 32 * g + 16 * h, x[0]);
-    load16(v + from + 32 * g + 16 * h, x[1]);
+  Group32<T> x[2];
+  if (src >= 0) {
+    x[0].load(k + from + 32 * g);
+    x[1].load(v + from + 32 * g);
   } else {
-#pragma unroll
-    for (int i = 0; i < 16; ++i) x[0][i] = x[1][i] = 0.f;
+    x[0].clear();
+    x[1].clear();
+  }
+  if (kept && g == 0 && s < cap) {
+    c.state.pos[o] = src;
+    c.state.acc[o] = src >= 0 ? attn_acc[(int64_t)u * sh.T + src] : 0.f;
+    c.state.vnorm[o] = src >= 0 ? vnorm[(int64_t)u * sh.T + src] : 0.f;
+    if (s == 0) {
+      c.state.len[u] = len;
+      c.state.free_slot[u] = len;
+      c.state.next_pos[u] = sh.T;
+      c.state.last_slot[u] = -1;
+    }
   }
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
-    float mn = x[t][0], mx = x[t][0];
-#pragma unroll
-    for (int i = 1; i < 16; ++i) { mn = fminf(mn, x[t][i]); mx = fmaxf(mx, x[t][i]); }
-    mn = fminf(mn, __shfl_xor_sync(0xffffffffu, mn, 1));
-    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+    float mn, mx;
+    x[t].range(mn, mx);
     const Q4Group q = q4_group(mn, mx);
-    if (from >= 0 && h == 0) reinterpret_cast<uint32_t*>(t ? c.v_params : c.k_params)[o * (HD / 32) + g] = q4_params(q);
-    unsigned char* row = stage[wid][t] + (lane / LPR) * (HD / 2);
+    if (src >= 0) reinterpret_cast<uint32_t*>(t ? c.v_params : c.k_params)[o * NG + g] = q4_params(q);
+    unsigned char* row = stage[wid][t] + (lane / NG) * (HD / 2);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      uint32_t code = 0;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) code |= q4_code(q, x[t][4 * j + e]) << (4 * e);
-      *reinterpret_cast<uint16_t*>(row + q4_byte<HD>(g, 4 * h + j)) = (uint16_t)code;
-    }
+    for (int j = 0; j < 8; ++j)
+      *reinterpret_cast<uint16_t*>(row + q4_byte<HD>(g, j)) = (uint16_t)q4_codes(q, x[t].at(4 * j), x[t].at(4 * j + 1), x[t].at(4 * j + 2), x[t].at(4 * j + 3));
   }
-  const uint32_t rows = __ballot_sync(0xffffffffu, from >= 0 && sub == 0);      // bit LPR * r: row r is live
-  __syncwarp();
-  const int t = lane >> 4, at = (lane & 15) * 16, r = at / (HD / 2);            // lanes 0-15 K, 16-31 V
-  if (rows >> (LPR * r) & 1u) {
-    unsigned char* dst = static_cast<unsigned char*>(t ? c.state.v_cache : c.state.k_cache) + ((int64_t)u * cap + first) * (HD / 2) + at;
-    *reinterpret_cast<uint4*>(dst) = *reinterpret_cast<const uint4*>(stage[wid][t] + at);
+  const uint32_t rows = __ballot_sync(0xffffffffu, src >= 0 && g == 0);           // bit NG * r: row r is live
+  const int at = lane * 16, r = at / (HD / 2);
+  if (rows >> (NG * r) & 1u) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      unsigned char* dst = static_cast<unsigned char*>(t ? c.state.v_cache : c.state.k_cache) + ((int64_t)u * cap + first) * (HD / 2) + at;
+      *reinterpret_cast<uint4*>(dst) = *reinterpret_cast<const uint4*>(stage[wid][t] + at);
+    }
   }
 }
 
@@ -111,11 +139,11 @@ __device__ __forceinline__ void store4(float* p, const float (&x)[4]) { *reinter
 // A lane takes HD / 16 bytes of a row, i.e. four channels of each of its groups; eight lanes a row.  A warp's stores of one group
 // cover four rows, 64 or 128 bytes each.
 template <typename T, int HD>
-__global__ void __launch_bounds__(PK_THREADS)
+__global__ void __launch_bounds__(UP_THREADS)
 unpack_q4_kernel(int64_t slots, vatp_cache_q4 c, T* k, T* v) {
   constexpr int G = HD / 32;
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  const int64_t i = (int64_t)blockIdx.x * (PK_THREADS / 8) + threadIdx.x / 8;    // the slot
+  const int64_t i = (int64_t)blockIdx.x * (UP_THREADS / 8) + threadIdx.x / 8;    // the slot
   const int j = threadIdx.x & 7;
   if (i >= slots || c.state.pos[i] < 0) return;
   uint32_t w[2][G / 2], pr[2][G];
@@ -163,7 +191,7 @@ __global__ void ring_q4_kernel(int T, int w, int B, int cap, const float* __rest
 template <typename T, int HD>
 cudaError_t pack_hd(const Shape& s, int B, const void* k, const void* v, const int32_t* kept, const int32_t* pos_from, const float* attn_acc,
                     const float* vnorm, const vatp_cache_q4& c, int32_t* dev_status, cudaStream_t st) {
-  constexpr int SLOTS = PK_WARPS * 512 / HD;       // of a CTA
+  constexpr int SLOTS = PK_WARPS * 1024 / HD;      // of a CTA
   const int cap = cache_capacity(B), per_unit = (cap + SLOTS - 1) / SLOTS;
   if ((int64_t)s.units * per_unit > 0x7fffffffll) return cudaErrorInvalidValue;
   DependentLaunch dl(dim3((unsigned)(s.units * per_unit)), dim3(PK_THREADS), 0, st);
@@ -172,9 +200,9 @@ cudaError_t pack_hd(const Shape& s, int B, const void* k, const void* v, const i
 
 template <typename T, int HD>
 cudaError_t unpack_hd(int units, int B, const vatp_cache_q4& c, void* k, void* v, cudaStream_t st) {
-  const int64_t slots = (int64_t)units * cache_capacity(B), ctas = (slots + PK_THREADS / 8 - 1) / (PK_THREADS / 8);
+  const int64_t slots = (int64_t)units * cache_capacity(B), ctas = (slots + UP_THREADS / 8 - 1) / (UP_THREADS / 8);
   if (ctas > 0x7fffffffll) return cudaErrorInvalidValue;
-  DependentLaunch dl(dim3((unsigned)ctas), dim3(PK_THREADS), 0, st);
+  DependentLaunch dl(dim3((unsigned)ctas), dim3(UP_THREADS), 0, st);
   return cudaLaunchKernelEx(&dl.cfg, unpack_q4_kernel<T, HD>, slots, c, (T*)k, (T*)v);
 }
 

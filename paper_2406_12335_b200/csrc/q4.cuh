@@ -20,10 +20,14 @@ __device__ __forceinline__ Q4Group q4_group(float mn, float mx) {
   g.inv = g.sc > 0.f ? __frcp_rn(g.sc) : 0.f;
   return g;
 }
-// rint((x - lo) / sc) in 0 .. 15, each operation rounded by itself.  (1.5 * 2^23 added: the code stands in the low bits)
-__device__ __forceinline__ uint32_t q4_code(const Q4Group& g, float x) {
-  const float y = fminf(__fmul_rn(__fsub_rn(x, g.lo), g.inv), 15.f);
-  return __float_as_uint(__fadd_rn(y, 12582912.f)) & 15u;
+// rint((x - lo) / sc) of four values, 0 .. 15 each (the scale is rounded up: 15 is not exceeded), each operation rounded by itself; the
+// four nibbles in the low half of the result, the first lowest.  Adding 1.5 * 2^23 rounds to the nearest integer, which then
+// stands in the low bits.
+__device__ __forceinline__ uint32_t q4_codes(const Q4Group& g, float x0, float x1, float x2, float x3) {
+  constexpr float M = 12582912.f;
+  const uint32_t c0 = __float_as_uint(__fadd_rn(__fmul_rn(__fsub_rn(x0, g.lo), g.inv), M)), c1 = __float_as_uint(__fadd_rn(__fmul_rn(__fsub_rn(x1, g.lo), g.inv), M));
+  const uint32_t c2 = __float_as_uint(__fadd_rn(__fmul_rn(__fsub_rn(x2, g.lo), g.inv), M)), c3 = __float_as_uint(__fadd_rn(__fmul_rn(__fsub_rn(x3, g.lo), g.inv), M));
+  return (c0 + 16u * c1) + 256u * (c2 + 16u * c3);       // (above the low half: whatever the float's upper bits add up to)
 }
 // a group's parameters as stored: the scale in the low half, the low end in the high half (both are bf16 values)
 __device__ __forceinline__ uint32_t q4_params(const Q4Group& g) {
@@ -46,7 +50,7 @@ __device__ __forceinline__ uint32_t q4_row(const float (&x)[4], uint32_t& params
   }
   const Q4Group g = q4_group(mn, mx);
   params = q4_params(g);
-  return q4_code(g, x[0]) | q4_code(g, x[1]) << 4 | q4_code(g, x[2]) << 8 | q4_code(g, x[3]) << 12;
+  return q4_codes(g, x[0], x[1], x[2], x[3]) & 0xffffu;
 }
 
 }  // namespace vatp
