@@ -6,7 +6,9 @@
 //   o_c = sum_i p_i lo_ig + sum_i (p_i sc_ig) code_ic
 // The sums over codes run on the warp-level tensor-core path (mma.sync m16n8k16, fp16 in, fp32 accumulate), the rest in fp32:
 //   * a code in the low bits of a 16-bit word IS the fp16 number code * 2^-24 (subnormal), one in bits 4-7 is code * 2^-20: unpacking
-//     is one AND per two codes and one shift per eight; the constant factors go into the other operand and the result;
+//     is one AND per two codes and one shift per eight; the constant factors go into the other operand and the result.  The tensor
+//     cores align such a product by its nominal exponent of -14 and cut off what lies 24 bits below: 4e-5 of an output of four heads
+//     x 2001 slots, which 16 bits do not show.  With fp32 inputs all codes are brought to bits 6-9 (code * 2^-18, a shift each);
 //   * the other operand's magnitude does not matter: q is scaled by a power of two per head, p_i sc_ig by one per warp and head that
 //     the largest of them determines.  bf16 inputs: q is exact in fp16, p_i sc_ig is rounded to its 11 bits (2^-12 of a term, an
 //     eighth of what the output's own rounding may be off by); fp32 inputs: both as a high half and a remainder, 2^-22;
@@ -116,6 +118,8 @@ __device__ __forceinline__ float exp2_fast(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+// 2^e, exactly; 2^127 beyond that, 0 below the normal numbers
+__device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)min(max(e + 127, 0), 254) << 23); }
 __device__ __forceinline__ float max_of(float x) {      // over the warp
   float y;
   asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
@@ -203,6 +207,12 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
   constexpr int N = GT > 4 ? 1 : 2;                             // tiles a warp works on at a time (with eight heads: registers)
   constexpr int PG = N == 2 ? NG : VW;                          // groups of a lane where p sc is formed: a slot or half of one
   constexpr int XS = INT ? NG * 4 * 2 * Q4_TILE : N * NG * XC * Q4_TILE * 2;      // bytes of a warp's second operand
+  // where a product takes the four codes of a 16-bit word: in place, then 8 bits down (SPLIT: each in bits 6-9)
+  constexpr int CODE_EXP = SPLIT ? 18 : 24;                     // a code in an even channel stands for code * 2^-CODE_EXP
+  auto codes0 = [](uint32_t x) { return SPLIT ? x << 6 & 0x03c003c0u : x & 0x000f000fu; };
+  auto codes1 = [](uint32_t x) { return SPLIT ? x << 2 & 0x03c003c0u : x & 0x00f000f0u; };
+  auto codes2 = [](uint32_t x) { return SPLIT ? x >> 2 & 0x03c003c0u : x >> 8 & 0x000f000fu; };
+  auto codes3 = [](uint32_t x) { return SPLIT ? x >> 6 & 0x03c003c0u : x >> 8 & 0x00f000f0u; };
   const int G = GT == 1 ? 1 : G_arg;
   // high half and remainder of head h: neighbours, i.e. in one lane's accumulators, or eight columns apart (two products)
   auto x_col = [](int h, int low) { return GT > 4 ? h + 8 * low : 2 * h + low; };
@@ -461,12 +471,12 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
         q_back[1] = q_back[0] * 256.f;
       } else {
         // q to [2^13, 2^14) by a power of two, as a high half and a remainder
-        const float up = __uint_as_float((uint32_t)(14 - ex + 127) << 23), back = __uint_as_float((uint32_t)(ex + 10 + 127) << 23) * scale_log2;
+        const float up = __uint_as_float((uint32_t)(14 - ex + 127) << 23), back = __uint_as_float((uint32_t)(ex + CODE_EXP - 14 + 127) << 23) * scale_log2;
 #pragma unroll
         for (int g = 0; g < NG; ++g)
 #pragma unroll
           for (int x = 0; x < 4; ++x) {
-            const float f = x & 1 ? up * 0.0625f : up, p0 = q[g][x] * f, p1 = q[g][x + 4] * f;      // (odd channels' codes stand four bits higher)
+            const float f = x & 1 && !SPLIT ? up * 0.0625f : up, p0 = q[g][x] * f, p1 = q[g][x + 4] * f;      // (odd channels' codes stand four bits higher)
             const __half2 h = __floats2half2_rn(p0, p1);
             qb[g][x] = *reinterpret_cast<const uint32_t*>(&h);
             if constexpr (SPLIT) qr[g][x] = half2_of(p0 - __low2float(h), p1 - __high2float(h));
@@ -588,14 +598,13 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
           for (int a = 0; a < N; ++a) {
             const uint32_t sel = g & 1 ? 0x7632u : 0x5410u;
             const uint32_t xa = __byte_perm(kw[2 * a][g >> 1], kw[2 * a][KW / 2 + (g >> 1)], sel), xb = __byte_perm(kw[2 * a + 1][g >> 1], kw[2 * a + 1][KW / 2 + (g >> 1)], sel);
-            const uint32_t ya = xa >> 8, yb = xb >> 8;
             float(&d)[4] = acc[a][g];
             d[0] = d[1] = d[2] = d[3] = 0.f;
-            mma_f16(d, xa & 0x000f000fu, xb & 0x000f000fu, xa & 0x00f000f0u, xb & 0x00f000f0u, qb[g][0], qb[g][1]);
-            mma_f16(d, ya & 0x000f000fu, yb & 0x000f000fu, ya & 0x00f000f0u, yb & 0x00f000f0u, qb[g][2], qb[g][3]);
+            mma_f16(d, codes0(xa), codes0(xb), codes1(xa), codes1(xb), qb[g][0], qb[g][1]);
+            mma_f16(d, codes2(xa), codes2(xb), codes3(xa), codes3(xb), qb[g][2], qb[g][3]);
             if constexpr (SPLIT) {
-              mma_f16(d, xa & 0x000f000fu, xb & 0x000f000fu, xa & 0x00f000f0u, xb & 0x00f000f0u, qr[g][0], qr[g][1]);
-              mma_f16(d, ya & 0x000f000fu, yb & 0x000f000fu, ya & 0x00f000f0u, yb & 0x00f000f0u, qr[g][2], qr[g][3]);
+              mma_f16(d, codes0(xa), codes0(xb), codes1(xa), codes1(xb), qr[g][0], qr[g][1]);
+              mma_f16(d, codes2(xa), codes2(xb), codes3(xa), codes3(xb), qr[g][2], qr[g][3]);
             }
           }
 #pragma unroll
@@ -650,11 +659,13 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
         o_acc[g][i][0] = o_acc[g][i][1] = o_acc[g][i][2] = o_acc[g][i][3] = 0.f;
         if (INT) o_int[g][i][0] = o_int[g][i][1] = o_int[g][i][2] = o_int[g][i][3] = 0;
       }
-    float m_own[GT], l_run[GT], lo_run[GT][PG];      // this warp's maxima; of this lane's slots (and groups): sum of p, sum of p lo
+    // this warp's maxima, rounded up to integers: p is taken relative to them, and what it is scaled by is a power of two (in one
+    // exponential with s, 2^29 p would have lost eight bits); of this lane's slots (and groups): sum of p, sum of p lo
+    float m_own[GT], l_run[GT], lo_run[GT][PG];
     int J[GT];
 #pragma unroll
     for (int h = 0; h < GT; ++h) {
-      m_own[h] = GT == 1 || h < G ? part_m[wid][h] : -INFINITY;
+      m_own[h] = GT == 1 || h < G ? ceilf(fminf(part_m[wid][h], 1e9f)) : -INFINITY;
       l_run[h] = 0.f;
       J[h] = -1000000000;
 #pragma unroll
@@ -735,7 +746,7 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
       for (int h = 0; h < GT; ++h)
         if (GT == 1 || h < G) {
           // (no live slot so far: m_own is -inf)
-          const float p = s[h] > -INFINITY ? exp2_fast(s[h] - m_own[h]) : 0.f, y = exp2_fast(s[h] - (float)(J[h] - 126 - X_TOP));
+          const float p = s[h] > -INFINITY ? exp2_fast(s[h] - m_own[h]) : 0.f, y = p * pow2((int)m_own[h] - (J[h] - 126 - X_TOP));
           l_run[h] += p;
 #pragma unroll
           for (int i = 0; i < PG; ++i) {
@@ -795,13 +806,12 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
             const uint2 b = *reinterpret_cast<const uint2*>(xh);
             const uint32_t sel = g & 1 ? 0x7632u : 0x5410u;
             const uint32_t xa = __byte_perm(vw[a][0][g >> 1], vw[a][1][g >> 1], sel), xb = __byte_perm(vw[a][2][g >> 1], vw[a][3][g >> 1], sel);
-            const uint32_t ya = xa >> 8, yb = xb >> 8;
-            mma_f16(o_acc[g][0], xa & 0x000f000fu, xa & 0x00f000f0u, xb & 0x000f000fu, xb & 0x00f000f0u, b.x, b.y);
-            mma_f16(o_acc[g][1], ya & 0x000f000fu, ya & 0x00f000f0u, yb & 0x000f000fu, yb & 0x00f000f0u, b.x, b.y);
+            mma_f16(o_acc[g][0], codes0(xa), codes1(xa), codes0(xb), codes1(xb), b.x, b.y);
+            mma_f16(o_acc[g][1], codes2(xa), codes3(xa), codes2(xb), codes3(xb), b.x, b.y);
             if constexpr (GT > 4 && SPLIT) {
               const uint2 d = *reinterpret_cast<const uint2*>(xh + 8 * Q4_TILE);
-              mma_f16(o_acc[g][0], xa & 0x000f000fu, xa & 0x00f000f0u, xb & 0x000f000fu, xb & 0x00f000f0u, d.x, d.y);
-              mma_f16(o_acc[g][1], ya & 0x000f000fu, ya & 0x00f000f0u, yb & 0x000f000fu, yb & 0x00f000f0u, d.x, d.y);
+              mma_f16(o_acc[g][0], codes0(xa), codes1(xa), codes0(xb), codes1(xb), d.x, d.y);
+              mma_f16(o_acc[g][1], codes2(xa), codes3(xa), codes2(xb), codes3(xb), d.x, d.y);
             }
           }
       }
@@ -826,11 +836,11 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
 #pragma unroll
     for (int h = 0; h < GT; ++h)
       if (GT == 1 || h < G) {
-        float m = m_own[h];
+        float m = part_m[0][h];
 #pragma unroll
-        for (int k = 0; k <= WARPS; ++k) m = fmaxf(m, part_m[k][h]);
+        for (int k = 1; k <= WARPS; ++k) m = fmaxf(m, part_m[k][h]);
         const bool any = m_own[h] > -INFINITY;
-        const float fm = any ? exp2_fast(m_own[h] - m) : 0.f, fj = any ? exp2_fast((float)(J[h] - 126 - X_TOP + (INT ? 0 : 24)) - m) : 0.f;
+        const float fm = any ? exp2_fast(m_own[h] - m) : 0.f, fj = any ? fm * pow2(J[h] - 126 - X_TOP + (INT ? 0 : CODE_EXP) - (int)m_own[h]) : 0.f;
 #pragma unroll
         for (int x = 0; x < 2; ++x)
           if ((GT > 4 ? 2 * t4 + x : t4) == h) fo[x] = fj;
@@ -858,9 +868,9 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
           if constexpr (INT) {
             o[i] = o_acc[g][0][i] + __shfl_xor_sync(0xffffffffu, o_acc[g][0][i], 1);      // (the upper digits' columns)
             o[i] *= fo[0];
-          } else {                           // the remainder's column beside the head's; codes in odd channels stand four bits higher
+          } else {                           // the remainder's column beside the head's
             o[i] = GT > 4 ? o_acc[g][i >> 1][2 * (i & 1) + x] : o_acc[g][i >> 1][2 * (i & 1)] + o_acc[g][i >> 1][2 * (i & 1) + 1];
-            o[i] *= i & 1 ? fo[x] * 0.0625f : fo[x];
+            o[i] *= i & 1 && !SPLIT ? fo[x] * 0.0625f : fo[x];
           }
         }
         if (h < G) *reinterpret_cast<float4*>(po + h * HD + 32 * g + 4 * r8) = make_float4(o[0], o[1], o[2], o[3]);

@@ -291,6 +291,76 @@ def test_steps_against_64_bits(b, h, kv, d, B, window, dtype, grow):
     _run_steps(p, _filled(p, n, seed=B + h), 5, dtype)
 
 
+@pytest.mark.parametrize("b,h,kv,d,B,window,dtype", [
+    (1, 32, 0, 128, 2048, 0, "bf16"),       # whole rounds of the warps and the incoming token's slot
+    (1, 32, 0, 64, 2055, 0, "f32"),         # ... and eight slots more
+    (1, 32, 0, 128, 2056, 0, "bf16"),       # ... one too many for that
+    (1, 32, 8, 128, 2050, 20, "bf16"),
+    (2, 70, 0, 64, 260, 0, "bf16"),
+    (1, 40, 0, 128, 3001, 0, "bf16"),       # CTAs of sixteen warps
+    (1, 40, 0, 64, 3001, 0, "f32"),
+    (1, 100, 0, 128, 1023, 30, "bf16"),     # ... each a unit of its own, with a history
+    (1, 160, 40, 128, 2500, 0, "bf16"),     # ... four heads
+    (1, 160, 40, 64, 2500, 5, "f32"),
+    (1, 240, 40, 128, 2500, 0, "bf16"),     # ... six heads
+    (1, 1600, 200, 128, 3000, 0, "bf16"),   # more units than SMs, eight heads: one CTA of sixteen warps on an SM
+    (2, 200, 0, 128, 700, 0, "f32"),
+])
+@pytest.mark.parametrize("grow", [0, 1500])
+def test_steps_of_every_division_of_a_unit(b, h, kv, d, B, window, dtype, grow):
+    p = _params(dtype, b, h, kv, d, B=B, F=2, R=3, window=window)
+    _run_steps(p, _filled(p, max(B - grow, 0), seed=B + h), 3, dtype)
+
+
+def test_integer_sums_of_more_slots_than_they_hold():
+    """More than 2048 slots of a warp: the integer sums are taken over in between."""
+    p = _params("bf16", 1, 150, 0, 64, B=17000)
+    c = _filled(p, 17000)
+    c.k_params[..., 0] *= 1e-3                                 # (logits near one another: all slots count)
+    c.v_codes.fill_(0xff)
+    _run_steps(p, c, 2, "bf16")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("kv", [0, 2, 1])
+@pytest.mark.parametrize("up", [True, False])
+def test_scales_that_grow_along_the_cache(dtype, kv, up):
+    """The power of two that p sc is scaled by moves again and again, or never after the first rows."""
+    p = _params(dtype, 1, 8, kv, 128, B=1100)
+    c = _filled(p, 1100)
+    grow = torch.exp2(torch.linspace(-30, 30, 1100, device="cuda")).bfloat16()
+    c.v_params[:, :, :1100] *= (grow if up else grow.flip(0))[:, None, None]
+    _run_steps(p, c, 3, dtype)
+
+
+@pytest.mark.parametrize("h,kv", [(8, 0), (8, 2)])
+def test_precision_of_32_bit_steps(h, kv):
+    """Typical errors, against the bounds of the other tests: logits up to 32 (in log2) have an ulp of 2^-19, half of which is
+    2^-20 ln 2 = 7e-7 of a probability at most; rounded sums and the exponential add less."""
+    V = P.vatp()
+    b, d, B = 1, 128, 2000
+    p = _params("f32", b, h, kv, d, B=B)
+    c = _filled(p, B)
+    hk = kv or h
+    c.k_params *= 0.5
+    ref = Q.State(c, d, B, 0, 0, p.scale)
+    g = _gen(3)
+    q, k, v = torch.randn(b, h, d, generator=g, device="cuda"), _rows(g, b, hk, d, dtype="f32"), _rows(g, b, hk, d, dtype="f32")
+    out, before = torch.empty_like(q), c.acc.double()
+    V.vatp_decode_step_q4(p, c, q, k, v, out)
+    torch.cuda.synchronize()
+    want, pm, _, _, _, v_mag = ref.step(q.view(hk, h // hk, d), k.view(hk, d), v.view(hk, d))
+    # grouped queries: sums of fp16 products.  The sixteen of a tile and what they are added to are cut off 2^-24 below the largest
+    # one's nominal magnitude, p sc 2^-14, while a code counts p sc 2^-18: 17 * 16 * 2^-24 of the tile's largest p sc, and the
+    # sum of those is at most sum p sc <= v_mag / 15
+    cut = 17 * 16 / 15 * 2.0 ** -24 * v_mag.norm() if kv else 0.0
+    assert (out.double().view(want.shape) - want).norm() <= 1e-6 * want.norm() + cut
+    got = (c.acc.double() - before).view(hk, -1)
+    got[torch.arange(hk), ref.free] = c.acc.double().view(hk, -1)[torch.arange(hk), ref.free]
+    # (the difference of two stored sums: a rounding of the sum, 2^-24 of it, comes on top)
+    assert (got - pm).norm() <= 1e-6 * pm.norm() + 2.0 ** -24 * before.norm()
+
+
 @pytest.mark.parametrize("norm", ["l1", "l2", "linf"])
 def test_norms_and_protected_tokens(norm):
     """Sinks and recent tokens stay although they are the least important; the incoming row's norm is that of the row as given."""
