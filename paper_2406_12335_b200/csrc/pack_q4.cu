@@ -3,6 +3,7 @@
 // Bound by memory where the number of instructions allows: a row of 128 bf16 channels is 256 bytes in one form and 80 in the other.
 // 256 units x 1639 slots: rows into 4 bits 45.4 us (6.25 TB/s, 0.96 of a copy's rate), gathered out of prompts of 8192 tokens 54.7 (rows
 // of 256 bytes anywhere), back 47.9.
+#include "cache_copy.cuh"
 #include "q4.cuh"
 
 namespace vatp {
@@ -10,6 +11,16 @@ namespace {
 
 constexpr int PK_WARPS = 2, PK_THREADS = PK_WARPS * 32;      // (8 warps a CTA, which end together: 256 units x 1639 slots 48.8 us, so 45.3)
 constexpr int UP_THREADS = 256;
+
+// CTA `i` of those that copy a state from a to c; false for i < 0 (a CTA that has rows to do).  The unit's words go with its first CTA.
+template <int THREADS>
+__device__ __forceinline__ bool copy_state(const CopyPlan& plan, int i, const vatp_cache& a, const vatp_cache& c) {
+  if (i < 0) return false;
+  const int u = i / plan.ctas, cta = i - u * plan.ctas;
+  if (cta == 0 && threadIdx.x == 0) copy_unit_words(a, u, c, u);
+  copy_words<THREADS>(plan, cta, u, [&](auto f) { f(u); });
+  return true;
+}
 
 // A group of a row as it is stored: its least and largest value, and each of them.
 template <typename T> struct Group32;
@@ -64,11 +75,13 @@ template <> struct Group32<float> {
 // group's parameters is done once.  The codes pass through 512 bytes of shared memory so that they leave as full 16-byte words.
 // (What bounds it is the number of instructions: with half a group a lane, 17 a value where this has 9.)
 // kept != nullptr (compaction): slot s of unit u takes row kept[u][s] of the prompt, and the decode state is initialised.
-// kept == nullptr (conversion): slot s takes slot s of the cache k, v where pos_from says that it holds a token.
-template <typename T, int HD>
+// kept == nullptr (conversion): slot s takes slot s of the cache k, v where its state `a` says that it holds a token; further CTAs copy
+// that state (STATE: plan; a kernel of its own, since its copies in flight take registers: 256 units x 1639 slots without them 45.4 us, in
+// one kernel 50.0; the way back 47.9 and 60.4).
+template <typename T, int HD, bool STATE>
 __global__ void __launch_bounds__(PK_THREADS)
-pack_q4_kernel(Shape sh, int B, int cap, int blocks_per_unit, const T* k, const T* v, const int32_t* kept, const int32_t* pos_from,
-               const float* attn_acc, const float* vnorm, vatp_cache_q4 c, int32_t* dev_status) {
+pack_q4_kernel(const __grid_constant__ CopyPlan plan, Shape sh, int B, int cap, int blocks_per_unit, const T* k, const T* v, const int32_t* kept,
+               vatp_cache a, const float* attn_acc, const float* vnorm, vatp_cache_q4 c, int32_t* dev_status) {
   constexpr int NG = HD / 32, ROWS = 32 / NG;                    // lanes a row, rows of a warp
   __shared__ __align__(16) unsigned char stage[PK_WARPS][2][512];
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
@@ -76,6 +89,8 @@ pack_q4_kernel(Shape sh, int B, int cap, int blocks_per_unit, const T* k, const 
   const int first = ((blockIdx.x - u * blocks_per_unit) * PK_WARPS + wid) * ROWS;      // this warp's first slot
   const int g = lane % NG, s = first + lane / NG;                 // this lane's group and slot
   asm volatile("griddepcontrol.wait;" ::: "memory");
+  if constexpr (STATE)
+    if (copy_state<PK_THREADS>(plan, blockIdx.x - sh.units * blocks_per_unit, a, c.state)) return;
   if (first >= cap) return;
   const int len = min(sh.T, B);
   const int64_t o = (int64_t)u * cap + s;
@@ -86,7 +101,7 @@ pack_q4_kernel(Shape sh, int B, int cap, int blocks_per_unit, const T* k, const 
     if (src >= 0 && !VATP_INB(src, sh.T, dev_status)) src = -1;
     from = unit_offset(sh, u) + (int64_t)src * sh.st;
   } else {
-    if (s < cap && pos_from[o] >= 0) src = s;
+    if (s < cap && a.pos[o] >= 0) src = s;
     from = o * HD;
   }
   Group32<T> x[2];
@@ -138,11 +153,15 @@ __device__ __forceinline__ void store4(float* p, const float (&x)[4]) { *reinter
 
 // A lane takes HD / 16 bytes of a row, i.e. four channels of each of its groups; eight lanes a row.  A warp's stores of one group
 // cover four rows, 64 or 128 bytes each.
-template <typename T, int HD>
+template <typename T, int HD, bool STATE>
 __global__ void __launch_bounds__(UP_THREADS)
-unpack_q4_kernel(int64_t slots, vatp_cache_q4 c, T* k, T* v) {
+unpack_q4_kernel(const __grid_constant__ CopyPlan plan, int row_ctas, int64_t slots, vatp_cache_q4 c, vatp_cache to) {
   constexpr int G = HD / 32;
   asm volatile("griddepcontrol.wait;" ::: "memory");
+  if constexpr (STATE)
+    if (copy_state<UP_THREADS>(plan, blockIdx.x - row_ctas, c.state, to)) return;
+  T* k = static_cast<T*>(to.k_cache);
+  T* v = static_cast<T*>(to.v_cache);
   const int64_t i = (int64_t)blockIdx.x * (UP_THREADS / 8) + threadIdx.x / 8;    // the slot
   const int j = threadIdx.x & 7;
   if (i >= slots || c.state.pos[i] < 0) return;
@@ -189,32 +208,39 @@ __global__ void ring_q4_kernel(int T, int w, int B, int cap, const float* __rest
 }
 
 template <typename T, int HD>
-cudaError_t pack_hd(const Shape& s, int B, const void* k, const void* v, const int32_t* kept, const int32_t* pos_from, const float* attn_acc,
-                    const float* vnorm, const vatp_cache_q4& c, int32_t* dev_status, cudaStream_t st) {
+cudaError_t pack_hd(const Shape& s, int B, const void* k, const void* v, const int32_t* kept, const CacheArray* arrays, int n, const vatp_cache& a,
+                    const float* attn_acc, const float* vnorm, const vatp_cache_q4& c, int32_t* dev_status, cudaStream_t st) {
   constexpr int SLOTS = PK_WARPS * 1024 / HD;      // of a CTA
   const int cap = cache_capacity(B), per_unit = (cap + SLOTS - 1) / SLOTS;
-  if ((int64_t)s.units * per_unit > 0x7fffffffll) return cudaErrorInvalidValue;
-  DependentLaunch dl(dim3((unsigned)(s.units * per_unit)), dim3(PK_THREADS), 0, st);
-  return cudaLaunchKernelEx(&dl.cfg, pack_q4_kernel<T, HD>, s, B, cap, per_unit, (const T*)k, (const T*)v, kept, pos_from, attn_acc, vnorm, c, dev_status);
+  CopyPlan plan;
+  if (!make_copy_plan(&plan, arrays, n, true, cap, cap, PK_THREADS)) return cudaErrorInvalidValue;
+  if (!plan.ctas && unit_words_apart(a, c.state)) plan.ctas = 1;
+  const int64_t ctas = (int64_t)s.units * ((int64_t)per_unit + plan.ctas);
+  if (ctas > 0x7fffffffll) return cudaErrorInvalidValue;
+  DependentLaunch dl(dim3((unsigned)ctas), dim3(PK_THREADS), 0, st);
+  return cudaLaunchKernelEx(&dl.cfg, plan.ctas ? pack_q4_kernel<T, HD, true> : pack_q4_kernel<T, HD, false>, plan, s, B, cap, per_unit, (const T*)k, (const T*)v, kept, a, attn_acc, vnorm, c, dev_status);
 }
 
 template <typename T, int HD>
-cudaError_t unpack_hd(int units, int B, const vatp_cache_q4& c, void* k, void* v, cudaStream_t st) {
-  const int64_t slots = (int64_t)units * cache_capacity(B), ctas = (slots + UP_THREADS / 8 - 1) / (UP_THREADS / 8);
-  if (ctas > 0x7fffffffll) return cudaErrorInvalidValue;
-  DependentLaunch dl(dim3((unsigned)ctas), dim3(UP_THREADS), 0, st);
-  return cudaLaunchKernelEx(&dl.cfg, unpack_q4_kernel<T, HD>, slots, c, (T*)k, (T*)v);
+cudaError_t unpack_hd(int units, int B, const vatp_cache_q4& c, const CacheArray* arrays, int n, const vatp_cache& to, cudaStream_t st) {
+  const int cap = cache_capacity(B);
+  const int64_t slots = (int64_t)units * cap, ctas = (slots + UP_THREADS / 8 - 1) / (UP_THREADS / 8);
+  CopyPlan plan;
+  if (!make_copy_plan(&plan, arrays, n, true, cap, cap, UP_THREADS)) return cudaErrorInvalidValue;
+  if (!plan.ctas && unit_words_apart(c.state, to)) plan.ctas = 1;
+  if (ctas + (int64_t)units * plan.ctas > 0x7fffffffll) return cudaErrorInvalidValue;
+  DependentLaunch dl(dim3((unsigned)(ctas + (int64_t)units * plan.ctas)), dim3(UP_THREADS), 0, st);
+  return cudaLaunchKernelEx(&dl.cfg, plan.ctas ? unpack_q4_kernel<T, HD, true> : unpack_q4_kernel<T, HD, false>, plan, (int)ctas, slots, c, to);
 }
 
 }  // namespace
 
-cudaError_t launch_pack_q4(const Shape& s, int dtype, int B, const void* k, const void* v, const int32_t* kept, const int32_t* pos_from,
-                           const float* attn_acc, const float* vnorm, const float* win_rows, const vatp_cache_q4& c,
-                           int32_t* dev_status, cudaStream_t st) {
+cudaError_t launch_compact_q4(const Shape& s, int dtype, int B, const void* k, const void* v, const int32_t* kept, const float* attn_acc,
+                              const float* vnorm, const float* win_rows, const vatp_cache_q4& c, int32_t* dev_status, cudaStream_t st) {
   auto f = dtype == VATP_F32 ? (s.d == 64 ? pack_hd<float, 64> : pack_hd<float, 128>)
                              : (s.d == 64 ? pack_hd<__nv_bfloat16, 64> : pack_hd<__nv_bfloat16, 128>);
-  cudaError_t e = f(s, B, k, v, kept, pos_from, attn_acc, vnorm, c, dev_status, st);
-  if (e == cudaSuccess && kept && s.window > 0) {
+  cudaError_t e = f(s, B, k, v, kept, nullptr, 0, c.state, attn_acc, vnorm, c, dev_status, st);
+  if (e == cudaSuccess && s.window > 0) {
     const int cap = cache_capacity(B);
     const int64_t ctas = (int64_t)s.units * ((cap + 127) / 128);
     if (ctas > 0x7fffffffll) return cudaErrorInvalidValue;
@@ -224,10 +250,21 @@ cudaError_t launch_pack_q4(const Shape& s, int dtype, int B, const void* k, cons
   return e;
 }
 
-cudaError_t launch_unpack_q4(int units, int d, int dtype, int B, const vatp_cache_q4& c, void* k, void* v, cudaStream_t st) {
+cudaError_t launch_pack_q4(int units, int d, int dtype, int B, const vatp_cache& from, const CacheArray* arrays, int n, const vatp_cache_q4& to,
+                           int32_t* dev_status, cudaStream_t st) {
+  Shape s;
+  memset(&s, 0, sizeof(s));
+  s.units = units;
+  s.heads = 1;
+  auto f = dtype == VATP_F32 ? (d == 64 ? pack_hd<float, 64> : pack_hd<float, 128>) : (d == 64 ? pack_hd<__nv_bfloat16, 64> : pack_hd<__nv_bfloat16, 128>);
+  return f(s, B, from.k_cache, from.v_cache, nullptr, arrays, n, from, nullptr, nullptr, to, dev_status, st);
+}
+
+cudaError_t launch_unpack_q4(int units, int d, int dtype, int B, const vatp_cache_q4& from, const CacheArray* arrays, int n, const vatp_cache& to,
+                             cudaStream_t st) {
   auto f = dtype == VATP_F32 ? (d == 64 ? unpack_hd<float, 64> : unpack_hd<float, 128>)
                              : (d == 64 ? unpack_hd<__nv_bfloat16, 64> : unpack_hd<__nv_bfloat16, 128>);
-  return f(units, B, c, k, v, st);
+  return f(units, B, from, arrays, n, to, st);
 }
 
 }  // namespace vatp

@@ -129,7 +129,7 @@ bool rows_apart(const void* a, int64_t a_bytes, const void* b, int64_t b_bytes) 
   return x >= y + (uintptr_t)b_bytes || y >= x + (uintptr_t)a_bytes;
 }
 
-// vatp_cache_pack_q4 (pack) and vatp_cache_unpack_q4: rows by one launch, then the state's arrays that are not shared
+// vatp_cache_pack_q4 (pack) and vatp_cache_unpack_q4
 vatp_status convert_q4(const vatp_params* p, const vatp_cache* wide, const vatp_cache_q4* narrow, bool pack, int32_t* dev_status, void* cuda_stream) {
   vatp_status s = check_params(p, false);
   if (s != VATP_OK) return s;
@@ -149,18 +149,8 @@ vatp_status convert_q4(const vatp_params* p, const vatp_cache* wide, const vatp_
   if (!pair.ok) return VATP_ERR_INVALID_ARG;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   decode_history_forget(st);
-  cudaError_t e;
-  if (pack) {
-    Shape sh;
-    std::memset(&sh, 0, sizeof(sh));
-    sh.units = (int)units;
-    sh.d = d;
-    e = launch_pack_q4(sh, p->dtype, p->budget, w[0], w[1], nullptr, from.pos, nullptr, nullptr, nullptr, *narrow, dev_status, st);
-  } else {
-    e = launch_unpack_q4((int)units, d, p->dtype, p->budget, *narrow, wide->k_cache, wide->v_cache, st);
-  }
-  if (e == cudaSuccess && pair.apart)
-    e = launch_cache_copy((int)units, kv_heads_of(p), p->batch, p->budget, p->budget, pair.a, pair.n, nullptr, false, from, to, dev_status, st);
+  const cudaError_t e = pack ? launch_pack_q4((int)units, d, p->dtype, p->budget, *wide, pair.a, pair.n, *narrow, dev_status, st)
+                             : launch_unpack_q4((int)units, d, p->dtype, p->budget, *narrow, pair.a, pair.n, *wide, st);
   return e == cudaSuccess ? VATP_OK : VATP_ERR_CUDA;
 }
 
@@ -433,7 +423,7 @@ vatp_status vatp_compact_q4(const vatp_params* p, const void* k, const void* v, 
   if (s != VATP_OK) return s;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   decode_history_forget(st);
-  const cudaError_t e = launch_pack_q4(sh, p->dtype, p->budget, k, v, kept_idx, nullptr, attn_acc, vnorm, win_rows, *cache, dev_status, st);
+  const cudaError_t e = launch_compact_q4(sh, p->dtype, p->budget, k, v, kept_idx, attn_acc, vnorm, win_rows, *cache, dev_status, st);
   return e == cudaSuccess ? VATP_OK : VATP_ERR_CUDA;
 }
 

@@ -178,15 +178,6 @@ cudaError_t launch_decode(const Shape& s, int dtype, int B, int F, int R, const 
 cudaError_t launch_decode_mma(const Shape& s, int B, int F, int R, const vatp_cache& c, const void* q, const void* k,
                               const void* v, void* out, int32_t* evicted, int32_t* dev_status, cudaStream_t st,
                               bool may_overlap, int G = 1);
-// 4-bit rows.  kept != nullptr: the prompt's kept rows and their state (with a history window from win_rows); else the rows of the slots
-// of k, v (a cache of the same budget) that pos_from says hold a token
-cudaError_t launch_pack_q4(const Shape& s, int dtype, int B, const void* k, const void* v, const int32_t* kept, const int32_t* pos_from,
-                           const float* attn_acc, const float* vnorm, const float* win_rows, const vatp_cache_q4& c,
-                           int32_t* dev_status, cudaStream_t st);
-cudaError_t launch_unpack_q4(int units, int d, int dtype, int B, const vatp_cache_q4& c, void* k, void* v, cudaStream_t st);
-// the generation step on 4-bit rows (G: query heads per KV head); cudaErrorNotSupported when the shape does not fit
-cudaError_t launch_decode_q4(int units, int G, int d, int dtype, int B, int F, int R, int window, int norm, float scale, const vatp_cache_q4& c,
-                             const void* q, const void* k, const void* v, void* out, int32_t* evicted, int32_t* dev_status, cudaStream_t st);
 // one array of a decode state and its counterpart: [units][rows][capacity] slots of slot_bytes bytes
 struct CacheArray {
   const void* from;
@@ -194,7 +185,18 @@ struct CacheArray {
   int rows, slot_bytes;
 };
 constexpr int MAX_CACHE_ARRAYS = 9;
-// src_of == nullptr: every entry from its own counterpart, arrays that both states share are left out
+// a prompt's kept rows into the 4-bit state, which is initialised (with a history window from win_rows)
+cudaError_t launch_compact_q4(const Shape& s, int dtype, int B, const void* k, const void* v, const int32_t* kept, const float* attn_acc,
+                              const float* vnorm, const float* win_rows, const vatp_cache_q4& c, int32_t* dev_status, cudaStream_t st);
+// a decode state into its 4-bit form and back: rows that hold a token, and the state's arrays (those that both share are left out)
+cudaError_t launch_pack_q4(int units, int d, int dtype, int B, const vatp_cache& from, const CacheArray* arrays, int n, const vatp_cache_q4& to,
+                           int32_t* dev_status, cudaStream_t st);
+cudaError_t launch_unpack_q4(int units, int d, int dtype, int B, const vatp_cache_q4& from, const CacheArray* arrays, int n, const vatp_cache& to,
+                             cudaStream_t st);
+// the generation step on 4-bit rows (G: query heads per KV head); cudaErrorNotSupported when the shape does not fit
+cudaError_t launch_decode_q4(int units, int G, int d, int dtype, int B, int F, int R, int window, int norm, float scale, const vatp_cache_q4& c,
+                             const void* q, const void* k, const void* v, void* out, int32_t* evicted, int32_t* dev_status, cudaStream_t st);
+// entry b of c becomes entry src_of[b] of a (in_place: both are the same state)
 cudaError_t launch_cache_copy(int units, int heads, int from_batch, int from_budget, int budget, const CacheArray* arrays, int n, const int32_t* src_of,
                               bool in_place, const vatp_cache& a, const vatp_cache& c, int32_t* dev_status, cudaStream_t st);
 // other work of this library was enqueued on the stream: the next decode launch waits for all of it

@@ -202,6 +202,26 @@ def test_conversion_over_shared_state():
     assert torch.equal(rows.k_cache[:, :, :50], Q.stored(a.k_cache[:, :, :50]).float().bfloat16())
 
 
+def test_conversion_with_only_the_units_words_apart():
+    """Every per-slot array shared, the words that count tokens not: those are copied."""
+    V, p = P.vatp(), _params(B=30, h=4)
+    a = _filled(p, 30, form="wide")
+    c = V.CacheQ4(p, share=a)
+    for name in ("len", "free_slot", "next_pos", "last_slot"):
+        setattr(c, name, torch.full_like(getattr(a, name), 77))
+    c.struct = V.CacheQ4Struct(c._struct(c.k_codes, c.v_codes), c.k_params.data_ptr(), c.v_params.data_ptr())
+    V.vatp_cache_pack_q4(p, a, c)
+    torch.cuda.synchronize()
+    for name in ("len", "free_slot", "next_pos", "last_slot"):
+        assert torch.equal(getattr(c, name), getattr(a, name)), name
+    for name in ("len", "free_slot", "next_pos", "last_slot"):
+        getattr(a, name).zero_()
+    V.vatp_cache_unpack_q4(p, c, a)
+    torch.cuda.synchronize()
+    for name in ("len", "free_slot", "next_pos", "last_slot"):
+        assert torch.equal(getattr(c, name), getattr(a, name)), name
+
+
 # ------------------------------------------------------------------------------------------------ generation
 def _run_steps(p, c, n_steps, dtype, *, seed=9):
     """n_steps steps of the call against 64 bits: outputs, the whole state, the released tokens, the stored rows."""
