@@ -36,7 +36,7 @@ def build(force: bool = False, verbose: bool = False, debug_bounds: bool = False
     lib = LIB_DEBUG if debug_bounds else LIB
     if not force and not is_stale(lib):
         return lib
-    cmd = [_nvcc(), "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
+    cmd = [_nvcc(), "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "--threads", "0",
            "-I", INCLUDE, "-shared", "-Xcompiler", "-fPIC", "-o", lib]
     if debug_bounds:
         cmd += ["-DVATP_DEBUG_BOUNDS"]

@@ -113,6 +113,16 @@ __device__ __forceinline__ void mma_u8(int (&d)[4], uint32_t a0, uint32_t a1, ui
   asm("mma.sync.aligned.m16n8k32.row.col.s32.u8.u8.s32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
       : "+r"(d[0]), "+r"(d[1]), "+r"(d[2]), "+r"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+// one lane of the warp
+__device__ __forceinline__ bool elected() {
+  uint32_t p;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "elect.sync _|p, 0xffffffff;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(p));
+  return p != 0;
+}
 __device__ __forceinline__ float exp2_fast(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -193,8 +203,9 @@ __device__ __forceinline__ unsigned long long min_key(unsigned long long key) {
 // logits [G][ld].
 template <int HD> constexpr int q4_item = Q4_ROWS * (HD / 2 + HD / 8);      // bytes of an item: codes, then parameters
 
-template <typename T, int HD, bool WINDOWED, int GT, int WARPS>
-__global__ void __launch_bounds__(WARPS * 32 + 32, WARPS == 8 ? 2 : 1)
+// ALONE: one CTA on an SM (eight warps then have 140 registers instead of 96: 32 units x 2049 slots 7.3 -> 6.8 us).
+template <typename T, int HD, bool WINDOWED, int GT, int WARPS, bool ALONE>
+__global__ void __launch_bounds__(WARPS * 32 + 32, ALONE ? 1 : 2)
 decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int cap, int F, int R, int w, int norm, float scale_log2, vatp_cache_q4 c, const T* q_new,
                  const T* k_new, const T* v_new, T* out, int32_t* evicted, int32_t* dev_status) {
   constexpr int WORKERS = WARPS * 32, THREADS = WORKERS + 32;   // warps that take slots, and one more
@@ -501,7 +512,9 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
     };
     auto release = [&]() {                    // every lane has read the item: its slot takes the next one
       __syncwarp();
-      if (next < 2 * n && lane == 0 && !bad) request(next, n, slot);
+      // (with one head per cache the elected lane's code takes registers that it does not have: 128 x 1025 slots 10.2 -> 11.0 us; with four
+      // heads 8 x 13108 18.0 -> 17.5)
+      if (next < 2 * n && (GT == 1 ? lane == 0 : elected())) request(next, n, slot);
       ++next;
       item += ITEM;
       if (++slot == depth) { slot = 0; item = ring; par ^= 1; }
@@ -1058,11 +1071,12 @@ cudaError_t launch_gt(int units, int G, int B, int F, int R, int window, int nor
   // Static arrays and what the system takes, rounded up (of a CTA of sixteen warps, of one of eight).
   constexpr size_t fixed16 = (GT > 4 ? 48 : GT > 1 ? 42 : 18) * 1024, fixed8 = (GT > 4 ? 29 : GT > 1 ? 25 : 11) * 1024;
   const bool win = window > 0;
-  auto kern16 = win ? decode_q4_kernel<T, HD, true, GT, 16> : decode_q4_kernel<T, HD, false, GT, 16>;
-  auto kern8 = win ? decode_q4_kernel<T, HD, true, GT, 8> : decode_q4_kernel<T, HD, false, GT, 8>;
+  auto kern16 = win ? decode_q4_kernel<T, HD, true, GT, 16, true> : decode_q4_kernel<T, HD, false, GT, 16, true>;
+  auto kern8 = win ? decode_q4_kernel<T, HD, true, GT, 8, true> : decode_q4_kernel<T, HD, false, GT, 8, true>;
+  auto pair8 = win ? decode_q4_kernel<T, HD, true, GT, 8, false> : decode_q4_kernel<T, HD, false, GT, 8, false>;
   const size_t most16 = 226 * 1024 - fixed16, most8 = 226 * 1024 - fixed8;
   // Units on fewer CTAs than SMs: an SM to a CTA (two of a launch on one SM while others idle: 32 units x 2049 slots, four CTAs each,
-  // 8.0 and 7.3 us per step), as many CTAs per unit as run at once and find some slots, of sixteen warps when there are more than
+  // 8.0 and 7.3 us per step, with the same kernel), as many CTAs per unit as run at once and find some slots, of sixteen warps when there are more than
   // three rounds for eight (74 units x 4097: 15.7 and 14.0 us; 32 x 1025: 6.0 and 6.8, which is why not always).  More units
   // than SMs: one CTA of eight warps each, two on an SM.
   int split = 1;
@@ -1093,7 +1107,7 @@ cudaError_t launch_gt(int units, int G, int B, int F, int R, int window, int nor
   size_t dyn = bytes(split, depth);
   if (dyn > most || (int64_t)units * split > 0x7fffffffll) return cudaErrorNotSupported;
   if (alone && dyn < 120 * 1024 - fixed8) dyn = 120 * 1024 - fixed8;
-  auto kern = warps == 16 ? kern16 : kern8;
+  auto kern = warps == 16 ? kern16 : alone ? kern8 : pair8;
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most);
   if (e == cudaSuccess && split > 8) e = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
   if (e != cudaSuccess) return e;
