@@ -13,7 +13,7 @@ namespace {
 constexpr int CC_THREADS = 128;
 
 __global__ void __launch_bounds__(CC_THREADS)
-cache_copy_kernel(const __grid_constant__ CopyPlan plan, int batch, int heads, int from_batch, int from_cap, int cap, int budget, int in_place, const int32_t* src_of,
+cache_copy_kernel(const __grid_constant__ CopyPlan plan, int batch, int heads, int from_batch, int from_cap, int from_budget, int cap, int budget, int in_place, const int32_t* src_of,
                   vatp_cache a, vatp_cache c, int32_t* dev_status) {
   const int unit = blockIdx.x / plan.ctas, b = unit / heads, head = unit - b * heads, tid = threadIdx.x, lane = tid & 31;
   int cta = blockIdx.x - unit * plan.ctas;
@@ -35,7 +35,7 @@ cache_copy_kernel(const __grid_constant__ CopyPlan plan, int batch, int heads, i
     fits = there == src || there == VATP_SEQ_KEEP;
   }
   const int v = fits ? src * heads + head : 0;
-  if (fits && from_cap > cap) fits = a.len[v] <= budget;
+  if (fits && from_budget > budget) fits = a.len[v] <= budget;
   if (!fits) {
     if (tid == 0 && dev_status) atomicExch(dev_status, (int)VATP_ERR_INVALID_ARG);
     return;
@@ -76,7 +76,7 @@ cudaError_t launch_cache_copy(int units, int heads, int from_batch, int from_bud
   CopyPlan plan;
   if (!make_copy_plan(&plan, arrays, n, false, fc, tc, CC_THREADS) || (int64_t)units * plan.ctas > 0x7fffffffll) return cudaErrorInvalidValue;
   DependentLaunch dl(dim3((unsigned)(units * plan.ctas)), dim3(CC_THREADS), 0, st);
-  return cudaLaunchKernelEx(&dl.cfg, cache_copy_kernel, plan, units / heads, heads, from_batch, fc, tc, budget, in_place ? 1 : 0, src_of, a, c, dev_status);
+  return cudaLaunchKernelEx(&dl.cfg, cache_copy_kernel, plan, units / heads, heads, from_batch, fc, from_budget, tc, budget, in_place ? 1 : 0, src_of, a, c, dev_status);
 }
 
 }  // namespace vatp

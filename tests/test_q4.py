@@ -635,6 +635,21 @@ def test_entries_that_do_not_fit_are_left_alone():
     assert torch.equal(dst.k_codes[1, :, :24], src.k_codes[1, :, :24]) and torch.all(dst.len[1] == 24)
 
 
+def test_budgets_of_equal_capacity_that_differ():
+    """Budgets of 70 and 66 have 72 slots each: a full entry of the larger one is too long for the smaller all the same."""
+    V = P.vatp()
+    pf, pt = _params(b=2, B=70), _params(b=2, B=66)
+    src, dst = _filled(pf, 70), _filled(pt, 66, seed=2)
+    assert src.cap == dst.cap
+    src.len[1], src.free_slot[1], src.pos[1, :, 66:] = 66, 66, -1
+    before, status = _clone(dst, pt), _status()
+    V.vatp_cache_copy(pt, src, dst, torch.tensor([0, 1], dtype=torch.int32, device="cuda"), dev_status=status)
+    torch.cuda.synchronize()
+    assert int(status) == 1
+    for name, t in _arrays(dst).items():
+        assert torch.equal(t[0], getattr(before, name)[0]) and torch.equal(t[1], getattr(src, name)[1]), name
+
+
 def test_a_freed_entry_and_a_joined_one_go_on_generating():
     """Freed: the cache starts anew.  Joined from a smaller budget: it grows to the larger one."""
     V = P.vatp()
