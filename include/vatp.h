@@ -331,7 +331,7 @@ vatp_status vatp_compact_q4(const vatp_params* params, const void* k, const void
  * A decode state with rows of the params dtype into one with 4-bit rows, and back (the rows' values, rounded to the params dtype
  * once).  Both states have params->batch entries and params->budget.  Rows of slots that hold a token are converted, others left
  * alone; all else of the state is copied, except for arrays that both structs share (a program that keeps both forms of the rows
- * over one set of acc, vnorm, pos, ... arrays): those stay as they are.  ring and acc_fixed must be 16-byte aligned.  Rows in the
+ * over one set of acc, vnorm, pos, ... arrays; a step on one form leaves the other's rows behind): those stay as they are.  ring and acc_fixed must be 16-byte aligned.  Rows in the
  * two forms may not overlap, nor may arrays overlap their counterparts without being the same (VATP_ERR_INVALID_ARG).
  * seq_len in params is ignored.
  */

@@ -4,16 +4,22 @@
 // With the values lo_ig + sc_ig code_ic of row i, group g and channel c:
 //   s_i = scale * sum_g ( sc_ig * sum_{c in g} q_c code_ic + lo_ig * sum_{c in g} q_c ),   p = softmax(s)
 //   o_c = sum_i p_i lo_ig + sum_i (p_i sc_ig) code_ic
-// The sums over codes run on the warp-level tensor-core path (mma.sync m16n8k16, fp16 in, fp32 accumulate), the rest in fp32:
-//   * a code in the low bits of a 16-bit word IS the fp16 number code * 2^-24 (subnormal), one in bits 4-7 is code * 2^-20: unpacking
-//     is one AND per two codes and one shift per eight; the constant factors go into the other operand and the result.  The tensor
-//     cores align such a product by its nominal exponent of -14 and cut off what lies 24 bits below: 4e-5 of an output of four heads
-//     x 2001 slots, which 16 bits do not show.  With fp32 inputs all codes are brought to bits 6-9 (code * 2^-18, a shift each);
-//   * the other operand's magnitude does not matter: q is scaled by a power of two per head, p_i sc_ig by one per warp and head that
-//     the largest of them determines.  bf16 inputs: q is exact in fp16, p_i sc_ig is rounded to its 11 bits (2^-12 of a term, an
-//     eighth of what the output's own rounding may be off by); fp32 inputs: both as a high half and a remainder, 2^-22;
-//   * rows are stored so that the 16 bytes a lane loads hold the channels it needs in an MMA operand, of every group: rows go from
-//     global memory into operand registers by plain 8- and 16-byte loads, without shared memory.
+// The sums over codes run on the warp-level tensor-core path, the rest in fp32.  How depends on the query heads of a unit:
+//   * one head (INT; mma.sync m16n8k32 in 8-bit integers, 32-bit sums): a byte of a row is lo + 16 hi, its upper half 16 hi after one AND,
+//     so the rows' words are operands as they are and unpacking is an instruction per eight codes.  The other operand has eight
+//     columns for one head: q is a 25-bit integer (a power of two takes the largest below 2^25), and lo q_lo + hi q_hi =
+//     byte * q_lo + upper half / 16 * (q_hi - 16 q_lo), each factor as four signed digits of 8 bits in columns of their own, two groups
+//     side by side.  p_i sc_ig is an integer below 2^29 in four unsigned digits.  All products are exact; a fp32 q loses 2^-25 of the
+//     largest, p sc 2^-29 of the warp's largest;
+//   * several heads (m16n8k16 in fp16, 32-bit sums; a column or two for each head): a code in the low bits of a 16-bit word IS the fp16
+//     number code * 2^-24 (subnormal), one in bits 4-7 is code * 2^-20: unpacking is one AND per two codes and one shift per eight;
+//     the constant factors go into the other operand and the result.  The tensor cores align such a product by its nominal
+//     exponent of -14 and cut off what lies 24 bits below: 4e-5 of an output of four heads x 2001 slots, which 16 bits do not show.
+//     With fp32 inputs all codes are brought to bits 6-9 (code * 2^-18, a shift each).  The other operand's magnitude does not matter:
+//     q is scaled by a power of two per head, p_i sc_ig by one per warp and head that the largest of them determines.  bf16 inputs: q is exact
+//     in fp16, p_i sc_ig is rounded to its 11 bits (2^-12 of a term, an eighth of what the output's own rounding may be off by); fp32
+//     inputs: both as a high half and a remainder, 2^-22;
+//   * rows are stored so that the 8 or 16 bytes a lane takes hold the channels it needs in an MMA operand, of every group.
 // A unit is split over a thread-block cluster; the slots of a CTA over eight or sixteen warps, 32 at a time.
 //   * An item of K or of V is 32 consecutive rows, two bulk copies (codes, parameters) into the warp's ring in shared memory.  As many
 //     as the ring holds are requested before the launch ahead has finished; the one row that it may have appended since (last_slot) is
@@ -22,6 +28,11 @@
 //   * One more warp takes the incoming token, which is no part of any item: it quantises and stores the rows and is a partial of its own.
 //   * The CTA joins its partials, the cluster those of its CTAs by st.async into the partners' shared memory; every CTA then updates the
 //     indicators of its own slots, and every warp sends its eviction candidate to rank 0.
+// What bounds it (one head, d 128): instructions and their latency, not memory.  An item's two products are 645 instructions of a warp
+// (110 of them requests) for 5 KB, and a step has some 1000 more per warp that do not depend on its length.  32 units x 2049 slots: 6.7 us
+// per step in a chain of steps, of which the launch takes 1.2, preparing q 0.75, two items' K 0.85, V 1.3, joining partials, CTAs and candidates 1.9;
+// 256 units x 1639: 18.7 us, 4.4 TB/s.  Not faster: a warp that requests all rings' items; three CTAs an SM (72 registers spill); p sc of the next
+// item formed while this one's products run (spills with eight warps in pairs: 18.7 -> 21.5 us; without spills 6.74 -> 6.97).
 #include <cooperative_groups.h>
 #include <cuda_fp16.h>
 
@@ -230,12 +241,12 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
   extern __shared__ __align__(128) unsigned char dyn[];
   const int ring_bytes = depth * ITEM;                          // of a warp
   float* new_o = reinterpret_cast<float*>(dyn + WARPS * ring_bytes);
-  float* logit_s = new_o + G * HD;
+  float* xo = new_o + G * HD;                                   // slices of partial outputs received [split][G][slice]
+  float* logit_s = xo + 2 * G * HD;
   // the second product's operand, [tile][group][column][slot] of fp16 or [group][digit][tile][slot] of bytes; slot s of a tile
   // stands at 4 (s mod 4) + s / 4
   __shared__ __align__(16) unsigned char xs[WARPS][XS];
   __shared__ float part_m[WARPS + 1][GT], part_l[WARPS + 1][GT], part_lo[WARPS][GT][NG];
-  __shared__ float xo[GT * HD];                                         // slices of partial outputs received [split][G][HD / split]
   __shared__ float2 ex_ml[Q4_SPLIT][GT];                                // per rank and head: maximum of its logits, sum of exp2(s - m)
   __shared__ float fr_s[Q4_SPLIT][GT], all_m[GT], all_inv[GT], new_norm_s;
   __shared__ Q4Candidate cand[Q4_SPLIT * WARPS];                     // in rank 0
@@ -245,6 +256,8 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
   const int tid = threadIdx.x, lane = tid & 31, wid = __shfl_sync(0xffffffffu, tid >> 5, 0);
   const int r8 = lane >> 2, t4 = lane & 3;
   const int u = blockIdx.x / split;
+  const int slice_log2 = (HD == 128 ? 7 : 6) - (31 - __clz(split)), slice = 1 << slice_log2;      // channels of the output that rank r < HD / slice writes
+  const bool writes = rank * slice < HD;
   // this CTA's slots of the unit: those of the tiles, and in the last CTA up to Q4_EXTRA more (see launch_gt)
   const int s0 = min(rank * chunk, cap), rows_alloc = min(chunk, cap - s0), rows_all = rank == split - 1 ? cap - s0 : rows_alloc;
   const int64_t base = (int64_t)u * cap + s0;
@@ -256,7 +269,7 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
   }
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   if (tid == WORKERS) {
-    bar_expect(s32(&ex_bar), (uint32_t)(8 * G * split + 4 * G * HD));
+    bar_expect(s32(&ex_bar), (uint32_t)(8 * G * split + (writes ? 4 * G * slice * split : 0)));
     if (rank == 0) bar_expect(s32(&cand_bar), (uint32_t)(split * WARPS * sizeof(Q4Candidate)));
   }
   if (!INT && wid < WARPS)      // (columns without a head stay 0)
@@ -894,7 +907,6 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
   if (split > 1) cluster_wait_acquire();
 
   // ---- to the unit's CTAs: maximum and sum to every one, channel slice r of the partial output to rank r
-  const int slice = HD / split, slice_log2 = 31 - __clz(slice);
   if (tid < split * G) {
     const int h = tid / split, dst = tid - h * split;
     float m = part_m[WARPS][h], l = part_l[WARPS][h];
@@ -927,7 +939,7 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
     inv_all = 1.f / __shfl_sync(0xffffffffu, L, 0);
   }
   if constexpr (GT == 1) {
-    if (wid * 32 < slice) {
+    if (writes && wid * 32 < slice) {
       float a = 0.f;
       for (int r = 0; r < split; ++r) a = fmaf(xo[r * slice + min(tid, slice - 1)], __shfl_sync(0xffffffffu, fr, r), a);
       if (tid < slice) to_out(out + (int64_t)u * HD + rank * slice + tid, a * inv_all);
@@ -938,7 +950,7 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
       if (lane == 0) { all_m[wid] = m_all; all_inv[wid] = inv_all; }
     }
     __syncthreads();
-    for (int i = tid; i < G * slice; i += THREADS) {
+    for (int i = tid; i < (writes ? G * slice : 0); i += THREADS) {
       const int h = i >> slice_log2, ch = i & (slice - 1);
       float a = 0.f;
       for (int r = 0; r < split; ++r) a = fmaf(xo[(r * G + h) * slice + ch], fr_s[r][h], a);
@@ -1037,10 +1049,10 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
 // once per device and size.
 template <typename Kernel>
 int clusters_at_once(Kernel kern, int split, int threads, size_t dyn) {
-  static std::atomic<int> known[16][5];
-  int dev = 0, log2 = 31 - __builtin_clz(split);
+  static std::atomic<int> known[16][Q4_SPLIT + 1];
+  int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return 0;
-  std::atomic<int>* entry = dev < 16 ? &known[dev][log2] : nullptr;
+  std::atomic<int>* entry = dev < 16 ? &known[dev][split] : nullptr;
   if (entry && entry->load()) return entry->load() - 1;
   if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)dyn) != cudaSuccess ||
       cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) {
@@ -1069,24 +1081,30 @@ cudaError_t launch_gt(int units, int G, int B, int F, int R, int window, int nor
   const int cap = cache_capacity(B), sms = device_sm_count();
   constexpr int ITEM = q4_item<HD>;
   // Static arrays and what the system takes, rounded up (of a CTA of sixteen warps, of one of eight).
-  constexpr size_t fixed16 = (GT > 4 ? 48 : GT > 1 ? 42 : 18) * 1024, fixed8 = (GT > 4 ? 29 : GT > 1 ? 25 : 11) * 1024;
+  constexpr size_t fixed16 = (GT > 4 ? 47 : GT > 1 ? 41 : 18) * 1024, fixed8 = (GT > 4 ? 28 : GT > 1 ? 24 : 11) * 1024;
   const bool win = window > 0;
   auto kern16 = win ? decode_q4_kernel<T, HD, true, GT, 16, true> : decode_q4_kernel<T, HD, false, GT, 16, true>;
   auto kern8 = win ? decode_q4_kernel<T, HD, true, GT, 8, true> : decode_q4_kernel<T, HD, false, GT, 8, true>;
   auto pair8 = win ? decode_q4_kernel<T, HD, true, GT, 8, false> : decode_q4_kernel<T, HD, false, GT, 8, false>;
   const size_t most16 = 226 * 1024 - fixed16, most8 = 226 * 1024 - fixed8;
   // Units on fewer CTAs than SMs: an SM to a CTA (two of a launch on one SM while others idle: 32 units x 2049 slots, four CTAs each,
-  // 8.0 and 7.3 us per step, with the same kernel), as many CTAs per unit as run at once and find some slots, of sixteen warps when there are more than
-  // three rounds for eight (74 units x 4097: 15.7 and 14.0 us; 32 x 1025: 6.0 and 6.8, which is why not always).  More units
+  // 8.0 and 7.3 us per step, with the same kernel), a power of two of them per unit that run at once and find some slots, of sixteen warps when there
+  // are more than three rounds for eight (74 units x 4097: 15.7 and 14.0 us; 32 x 1025: 6.0 and 6.8, which is why not always).  More units
   // than SMs: one CTA of eight warps each, two on an SM.
   int split = 1;
   while (split < Q4_SPLIT && units * split * 2 <= sms && cap / split >= 4 * Q4_ROWS && clusters_at_once(kern16, split * 2, 17 * 32, most16) >= units) split *= 2;
+  // Then any other number that saves the warps a round: clusters lie within a GPC, seven of sixteen CTAs run at once, fifteen of eight, but
+  // eleven of ten, 22 of six (16 units x 4002 slots, four heads: four CTAs each 12.8 us per step, six 10.7; 40 x 2049: two 9.1, three 7.7).
+  // Of clusters of three and of five, the last two of those said to fit have been seen to wait (of three, 43 units 7.7 us and 45 10.4).
+  auto rounds_of = [&](int split) { return (B + 1 - Q4_EXTRA + 8 * Q4_ROWS * split - 1) / (8 * Q4_ROWS * split); };
+  for (int more = split + 1; more <= Q4_SPLIT && units * more <= sms; ++more)
+    if (rounds_of(more) < rounds_of(split) && clusters_at_once(kern16, more, 17 * 32, most16) >= units + (more & 1) * 2) split = more;
   const bool alone = units <= sms;
   // a ring takes the warp's partial output in the end
   const int least = (G * HD * 4 + ITEM - 1) / ITEM > 2 ? (G * HD * 4 + ITEM - 1) / ITEM : 2;
   auto chunk_of = [&](int split) { return ((cap + split - 1) / split + Q4_ROWS - 1) / Q4_ROWS * Q4_ROWS; };
   int warps = 8;
-  auto bytes = [&](int split, int depth) { return (size_t)warps * depth * ITEM + (size_t)G * HD * 4 + (size_t)G * (chunk_of(split) + 2 * Q4_EXTRA) * 4; };
+  auto bytes = [&](int split, int depth) { return (size_t)warps * depth * ITEM + (size_t)G * HD * 12 + (size_t)G * (chunk_of(split) + 2 * Q4_EXTRA) * 4; };
   const size_t half = 113 * 1024 - fixed8;
   if (alone ? (cap + split - 1) / split > 3 * 8 * Q4_ROWS : bytes(split, least) > half) warps = 16;      // (half: two CTAs on an SM)
   const size_t most = warps == 16 ? most16 : most8;

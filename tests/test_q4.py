@@ -332,6 +332,14 @@ def test_steps_of_every_division_of_a_unit(b, h, kv, d, B, window, dtype, grow):
     _run_steps(p, _filled(p, max(B - grow, 0), seed=B + h), 3, dtype)
 
 
+@pytest.mark.parametrize("units,B,window", [(13, 4500, 0), (16, 4001, 0), (16, 3001, 9), (23, 4600, 0), (8, 13107, 0), (40, 1100, 0), (8, 5000, 40)])
+@pytest.mark.parametrize("G,d,dtype", [(1, 128, "bf16"), (1, 64, "f32"), (2, 64, "bf16"), (4, 128, "f32"), (4, 128, "bf16"), (8, 128, "bf16")])
+def test_units_over_odd_numbers_of_CTAs(units, B, window, G, d, dtype):
+    """Where fewer clusters of the next power of two run at once than there are units: three, five, six, nine or ten CTAs a unit."""
+    p = _params(dtype, 1, units * G, units if G > 1 else 0, d, B=B, F=2, R=3, window=window)
+    _run_steps(p, _filled(p, B, seed=B + G), 3, dtype)
+
+
 def test_integer_sums_of_more_slots_than_they_hold():
     """More than 2048 slots of a warp: the integer sums are taken over in between."""
     p = _params("bf16", 1, 150, 0, 64, B=17000)
