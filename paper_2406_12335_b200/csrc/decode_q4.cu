@@ -1107,6 +1107,8 @@ cudaError_t launch_gt(int units, int G, int B, int F, int R, int window, int nor
   auto bytes = [&](int split, int depth) { return (size_t)warps * depth * ITEM + (size_t)G * HD * 12 + (size_t)G * (chunk_of(split) + 2 * Q4_EXTRA) * 4; };
   const size_t half = 113 * 1024 - fixed8;
   if (alone ? (cap + split - 1) / split > 3 * 8 * Q4_ROWS : bytes(split, least) > half) warps = 16;      // (half: two CTAs on an SM)
+  // (rather eight warps than more CTAs than SMs where the logits leave no room for sixteen rings: 32 units x 13001 slots, eight heads: 95 -> 55 us)
+  if (alone && warps == 16 && bytes(split, least) > most16) warps = 8;
   const size_t most = warps == 16 ? most16 : most8;
   while (split < Q4_SPLIT && bytes(split, least) > most) split *= 2;      // (the logits of a CTA's slots stand in shared memory)
   int chunk = chunk_of(split), ld = chunk;
