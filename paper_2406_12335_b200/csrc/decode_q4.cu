@@ -31,7 +31,7 @@
 // What bounds it (one head, d 128): instructions and their latency, not memory.  An item's two products are 645 instructions of a warp
 // (110 of them requests) for 5 KB, and a step has some 1000 more per warp that do not depend on its length.  32 units x 2049 slots: 6.7 us
 // per step in a chain of steps, of which the launch takes 1.2, preparing q 0.75, two items' K 0.85, V 1.3, joining partials, CTAs and candidates 1.9;
-// 256 units x 1639: 18.7 us, 4.4 TB/s.  Not faster: a warp that requests all rings' items; three CTAs an SM (72 registers spill); p sc of the next
+// 256 units x 1639: 18.3 us, 4.0 TB/s.  Not faster: a warp that requests all rings' items; three CTAs an SM (72 registers spill); p sc of the next
 // item formed while this one's products run (spills with eight warps in pairs: 18.7 -> 21.5 us; without spills 6.74 -> 6.97).
 #include <cooperative_groups.h>
 #include <cuda_fp16.h>
@@ -1110,7 +1110,7 @@ cudaError_t launch_gt(int units, int G, int B, int F, int R, int window, int nor
   // (rather eight warps than more CTAs than SMs where the logits leave no room for sixteen rings: 32 units x 13001 slots, eight heads: 95 -> 55 us)
   if (alone && warps == 16 && bytes(split, least) > most16) warps = 8;
   const size_t most = warps == 16 ? most16 : most8;
-  while (split < Q4_SPLIT && bytes(split, least) > most) split *= 2;      // (the logits of a CTA's slots stand in shared memory)
+  while (split < Q4_SPLIT && bytes(split, least) > most) split = split * 2 < Q4_SPLIT ? split * 2 : Q4_SPLIT;      // (the logits of a CTA's slots stand in shared memory)
   int chunk = chunk_of(split), ld = chunk;
   // A few slots more than whole rounds of the warps (the incoming token's, where the budget fills them): the last warp of the last
   // CTA takes them.

@@ -340,6 +340,18 @@ def test_units_over_odd_numbers_of_CTAs(units, B, window, G, d, dtype):
     _run_steps(p, _filled(p, B, seed=B + G), 3, dtype)
 
 
+def test_the_longest_caches_of_eight_heads():
+    """Nine CTAs a unit, whose logits do not fit: sixteen, the most there are; beyond that the call is refused."""
+    V, p = P.vatp(), _params("bf16", 1, 64, 8, 128, B=45000, F=2, R=3)
+    _run_steps(p, _filled(p, 45000), 2, "bf16")
+    p = _params("bf16", 1, 64, 8, 128, B=200000, F=2, R=3)
+    c = V.CacheQ4(p)
+    q = torch.zeros(1, 64, 128, dtype=torch.bfloat16, device="cuda")
+    k = torch.zeros(1, 8, 128, dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(V.VatpError, match="unsupported"):
+        V.vatp_decode_step_q4(p, c, q, k, k, torch.empty_like(q))
+
+
 def test_integer_sums_of_more_slots_than_they_hold():
     """More than 2048 slots of a warp: the integer sums are taken over in between."""
     p = _params("bf16", 1, 150, 0, 64, B=17000)
