@@ -168,20 +168,30 @@ template <int N> __device__ __forceinline__ void words_of(const unsigned char* p
   }
 }
 
-// eight or four consecutive channels of a new row
-__device__ __forceinline__ void load_new(const __nv_bfloat16* p, float (&x)[8]) {
-  const uint4 r = load_behind_wait(reinterpret_cast<const uint4*>(p));
-  const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+// eight consecutive channels of q as they lie in memory, and as floats
+template <typename T> struct Raw8 {
+  uint4 r[sizeof(T) / 2];
+  __device__ __forceinline__ void load(const T* p) {
 #pragma unroll
-  for (int k = 0; k < 4; ++k) { x[2 * k] = __uint_as_float(w[k] << 16); x[2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u); }
-}
-__device__ __forceinline__ void load_new(const float* p, float (&x)[8]) {
-#pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    const float4 r = load_behind_wait(reinterpret_cast<const float4*>(p) + k);
-    x[4 * k] = r.x; x[4 * k + 1] = r.y; x[4 * k + 2] = r.z; x[4 * k + 3] = r.w;
+    for (int k = 0; k < (int)sizeof(T) / 2; ++k) r[k] = load_behind_wait(reinterpret_cast<const uint4*>(p) + k);
   }
-}
+  __device__ __forceinline__ void get(float (&x)[8]) const {
+#pragma unroll
+    for (int k = 0; k < (int)sizeof(T) / 2; ++k) {
+      const uint32_t w[4] = {r[k].x, r[k].y, r[k].z, r[k].w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (sizeof(T) == 4) {
+          x[4 * k + i] = __uint_as_float(w[i]);
+        } else {
+          x[2 * i] = __uint_as_float(w[i] << 16);
+          x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        }
+      }
+    }
+  }
+};
+// four consecutive channels of a new row
 __device__ __forceinline__ void load_new(const __nv_bfloat16* p, float (&x)[4]) {
   const uint2 r = *reinterpret_cast<const uint2*>(p);
   x[0] = __uint_as_float(r.x << 16); x[1] = __uint_as_float(r.x & 0xffff0000u);
@@ -298,7 +308,7 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
     bulk_load(dst, (is_v ? vc : kc) + (uint64_t)r0 * CODES, rows * CODES, bar);
     bulk_load(dst + Q4_ROWS * CODES, (is_v ? vp : kp) + (uint64_t)r0 * PARAMS, rows * PARAMS, bar);
   };
-  const int n_alloc = wid < WARPS ? items_in(rows_alloc) : 0, early = min(depth, 2 * n_alloc);
+  const int n_alloc = wid < WARPS ? items_in(rows_alloc) : 0, early = min(depth, n_alloc), ahead = min(depth, 2 * n_alloc);
   if (lane == 0)
     for (int j = 0; j < early; ++j) request(j, n_alloc, j);
   __syncwarp();
@@ -306,6 +316,19 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
   // Nothing but K and V rows is read before the previous launch has completed.
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int len_m = c.state.len[u], fs_m = c.state.free_slot[u], t = c.state.next_pos[u], ls = c.state.last_slot[u];
+  // q for the B operand of K q^T, requested along with the words above.  Lane (n = r8, t4): channels 8 t4 .. 8 t4 + 7 of groups of its column.
+  // INT: columns 0 - 3 are the four digits of group 0 (then of group 2), columns 4 - 7 of group 1 (3).  Else: column n is head n.
+  constexpr int QG = INT ? NG / 2 : NG;      // (INT: every second group)
+  Raw8<T> q_raw[QG];
+  if (wid < WARPS) {
+    const T* qp = q_new + ((int64_t)u * G + (INT ? 0 : min(r8, G - 1))) * HD + 32 * (INT ? r8 >> 2 : 0) + 8 * t4;
+#pragma unroll
+    for (int g = 0; g < QG; ++g) q_raw[g].load(qp + (INT ? 64 : 32) * g);
+    // the ring's first items of V, while these loads are under way
+    if (lane == 0)
+      for (int j = early; j < ahead; ++j) request(j, n_alloc, j);
+    __syncwarp();
+  }
 
   if (wid == WARPS) {
     // ---- the last warp: the incoming token.  Lane l < HD / 4 has channels 4 l .. 4 l + 3.
@@ -438,18 +461,24 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
   };
 
   if (wid < WARPS) {
-    // ---- B operand of K q^T.  Lane (n = r8, t4): channels 8 t4 .. 8 t4 + 7 of groups of its column.
-    // INT: columns 0 - 3 are the four digits of group 0 (then of group 2), columns 4 - 7 of group 1 (3).  Else: column n is head n.
+    // ---- the row that the launch ahead appended, if one of this warp's early items of K holds it
+    const int n = items_in(cnt_t);
+    int ls_item = -1;                         // that item
+    uint32_t ls_word = 0u;                    // that row (lanes below CODES / 4: codes, then parameters)
+    if (n == n_alloc && ls >= 0 && ls != fs && ls_local >= 0 && ls_local < cnt_t && ls_local / Q4_ROWS % WARPS == wid) {
+      ls_item = ls_local / (Q4_ROWS * WARPS);
+      if (lane < CODES / 4) ls_word = load_fresh(reinterpret_cast<const uint32_t*>(kc + (int64_t)ls_local * CODES) + lane);
+      else if (lane < CODES / 4 + NG) ls_word = load_fresh(reinterpret_cast<const uint32_t*>(kp + (int64_t)ls_local * PARAMS) + (lane - CODES / 4));
+    }
+
+    // ---- B operand of K q^T
     uint32_t qb[NG][INT ? 2 : 4], qr[GT > 1 && SPLIT ? NG : 1][4];
     // what a sum is to be multiplied by (INT: of the lane's two digits); sums of q over groups, * scale
     float q_back[2], qsum[INT ? NG / 2 : NG][2];
     {
-      constexpr int QG = INT ? NG / 2 : NG;
-      const int g0 = INT ? r8 >> 2 : 0;      // (then every second group)
-      const T* qp = q_new + ((int64_t)u * G + (INT ? 0 : min(r8, G - 1))) * HD + 32 * g0 + 8 * t4;
       float q[QG][8], most = 0.f, gs[QG];
 #pragma unroll
-      for (int g = 0; g < QG; ++g) load_new(qp + (INT ? 64 : 32) * g, q[g]);
+      for (int g = 0; g < QG; ++g) q_raw[g].get(q[g]);
 #pragma unroll
       for (int g = 0; g < QG; ++g) {
         gs[g] = 0.f;
@@ -463,7 +492,9 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
         gs[g] *= scale_log2;
       }
 #pragma unroll
-      for (int o = 1; o < (INT ? 32 : 4); o <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+      for (int o = 1; o < 4; o <<= 1)
+        if (!INT) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+      if (INT) most = max_of(most);
       const int ex = min(max((int)(__float_as_uint(most) >> 23) - 126, -90), 100);      // 2^ex is above the largest magnitude
       if constexpr (INT) {
         // Q = q 2^(25 - ex) as an integer; byte lo + 16 hi of a row by 16 Q_lo, its upper half 16 hi by Q_hi - 16 Q_lo
@@ -516,8 +547,7 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
     }
 
     // ---- the ring: the next item's slot, place and the parity of its barrier; the next item to request
-    const int n = items_in(cnt_t);
-    int slot = 0, next = early;
+    int slot = 0, next = ahead;
     uint32_t par = 0;
     const unsigned char* item = ring;
     auto arrived = [&]() {
@@ -532,22 +562,13 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
       item += ITEM;
       if (++slot == depth) { slot = 0; item = ring; par ^= 1; }
     };
-    int ls_item = -1;                         // the early item of K that holds the row which the launch ahead appended
-    uint32_t ls_word[2] = {0u, 0u};           // that row (lanes below CODES / 4: codes, then parameters) of K and of V
     if (n != n_alloc) {                       // fewer tokens than there is room for: what was requested early is dropped
       next = 2 * n;
-      for (int j = 0; j < early; ++j) { arrived(); release(); }
+      for (int j = 0; j < ahead; ++j) { arrived(); release(); }
       next = min(depth, 2 * n);
       if (lane == 0 && !bad)
         for (int j = 0; j < next; ++j) request(j, n, (slot + j) % depth);
       __syncwarp();
-    } else if (ls >= 0 && ls != fs && ls_local >= 0 && ls_local < cnt_t && ls_local / Q4_ROWS % WARPS == wid) {
-      ls_item = ls_local / (Q4_ROWS * WARPS);
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        if (lane < CODES / 4) ls_word[x] = load_fresh(reinterpret_cast<const uint32_t*>((x ? vc : kc) + (int64_t)ls_local * CODES) + lane);
-        else if (lane < CODES / 4 + NG) ls_word[x] = load_fresh(reinterpret_cast<const uint32_t*>((x ? vp : kp) + (int64_t)ls_local * PARAMS) + (lane - CODES / 4));
-      }
     }
     auto patch = [&](int j, uint32_t word) {  // item j of the ring
       if (j < early) {
@@ -655,7 +676,7 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
     };
     for (int j = 0; j < n; ++j) {
       arrived();
-      if (j == ls_item) patch(j, ls_word[0]);
+      if (j == ls_item) patch(j, ls_word);
       const int r0 = item_row(j);
 #pragma unroll 1
       for (int a = 0; a < 2; a += N) k_rows(r0 + a * Q4_TILE, a);
@@ -665,7 +686,9 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
 #pragma unroll
     for (int x = 0; x < MX; ++x) {
 #pragma unroll
-      for (int o = INT ? 1 : 4; o < 32; o <<= 1) m_run[x] = fmaxf(m_run[x], __shfl_xor_sync(0xffffffffu, m_run[x], o));
+      for (int o = 4; o < 32; o <<= 1)
+        if (!INT) m_run[x] = fmaxf(m_run[x], __shfl_xor_sync(0xffffffffu, m_run[x], o));
+      if (INT) m_run[x] = max_of(m_run[x]);
       const int h = GT > 1 ? 2 * t4 + x : 0;
       if (r8 == 0 && (GT > 1 ? h < G : t4 == 0)) part_m[wid][h] = m_run[x];
     }
@@ -846,7 +869,6 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
     for (int j = 0; !last; ++j) {
       if (j < n) {
         arrived();
-        if (j == ls_item) patch(n + j, ls_word[1]);
       }
       last = j == n;
       if (last && !INT) break;
