@@ -146,6 +146,19 @@ __device__ __forceinline__ float max_of(float x) {      // over the warp
   asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
   return y;
 }
+// NV values of every lane summed over the lanes that agree in what lies below LOW: lane l gets the sum of v[l / (32 / NV)] in v[0].
+// (Lanes halve the values between them as they go: 16 values take 16 shuffles, of which an SM does one per cycle, instead of 80.)
+template <int NV, int LOW> __device__ __forceinline__ void sum_over(float (&v)[NV], int lane) {
+  int o = 16;
+#pragma unroll
+  for (int half = NV / 2; half > 0; half /= 2, o /= 2) {
+    const bool up = lane & o;
+#pragma unroll
+    for (int i = 0; i < half; ++i) v[i] = (up ? v[i + half] : v[i]) + __shfl_xor_sync(0xffffffffu, up ? v[i] : v[i + half], o);
+  }
+#pragma unroll
+  for (; o >= LOW; o /= 2) v[0] += __shfl_xor_sync(0xffffffffu, v[0], o);
+}
 __device__ __forceinline__ uint32_t half2_of(float lo, float hi) {
   const __half2 h = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&h);
@@ -880,30 +893,42 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
     // (codes in odd channels stand four bits higher), into the ring
     if (!bad && !bar_wait(s32(&k_done), 0)) bad = true;
     __syncwarp();
-    float fo[2] = {0.f, 0.f};                // of this lane's columns
+    constexpr int COLS = GT > 4 ? 2 : 1;     // heads of this lane's columns of the accumulators: 2 t4 + x or t4
+    float fm[COLS], fo[COLS];                // factors of its sums of p and of its outputs
 #pragma unroll
-    for (int h = 0; h < GT; ++h)
-      if (GT == 1 || h < G) {
-        float m = part_m[0][h];
+    for (int x = 0; x < COLS; ++x) {
+      const int hc = GT == 1 ? 0 : COLS * t4 + x;
+      float mo = m_own[0], m = part_m[0][hc];
+      int j = J[0];
 #pragma unroll
-        for (int k = 1; k <= WARPS; ++k) m = fmaxf(m, part_m[k][h]);
-        const bool any = m_own[h] > -INFINITY;
-        const float fm = any ? exp2_fast(m_own[h] - m) : 0.f, fj = any ? fm * pow2(J[h] - 126 - X_TOP + (INT ? 0 : CODE_EXP) - (int)m_own[h]) : 0.f;
+      for (int h = 1; h < GT; ++h)
+        if (h == hc) { mo = m_own[h]; j = J[h]; }
 #pragma unroll
-        for (int x = 0; x < 2; ++x)
-          if ((GT > 4 ? 2 * t4 + x : t4) == h) fo[x] = fj;
+      for (int k = 1; k <= WARPS; ++k) m = fmaxf(m, part_m[k][hc]);
+      const bool any = hc < G && mo > -INFINITY;
+      fm[x] = any ? exp2_fast(mo - m) : 0.f;
+      fo[x] = any ? fm[x] * pow2(j - 126 - X_TOP + (INT ? 0 : CODE_EXP) - (int)mo) : 0.f;
+    }
+    {
+      constexpr int LOW = N == 2 ? 1 : 2;    // (neighbouring lanes have halves of a slot's groups with N == 1)
+      sum_over<GT, LOW>(l_run, lane);
+      float lo_all[GT * PG];
 #pragma unroll
-        for (int o = N == 2 ? 1 : 2; o < 32; o <<= 1) {
-          l_run[h] += __shfl_xor_sync(0xffffffffu, l_run[h], o);
+      for (int h = 0; h < GT; ++h)
 #pragma unroll
-          for (int i = 0; i < PG; ++i) lo_run[h][i] += __shfl_xor_sync(0xffffffffu, lo_run[h][i], o);
-        }
-        if (lane < (N == 2 ? 1 : 2)) {
-          if (lane == 0) part_l[wid][h] = l_run[h] * fm;
-#pragma unroll
-          for (int i = 0; i < PG; ++i) part_lo[wid][h][my_group + i] = lo_run[h][i] * fm;
-        }
+        for (int i = 0; i < PG; ++i) lo_all[h * PG + i] = lo_run[h][i];
+      sum_over<GT * PG, LOW>(lo_all, lane);
+      constexpr int L_LANES = 32 / GT, LO_LANES = 32 / (GT * PG);
+      const int hl = lane / L_LANES, ho = lane / LO_LANES / PG, io = lane / LO_LANES % PG;
+      float fl = __shfl_sync(0xffffffffu, fm[0], hl / COLS), fi = __shfl_sync(0xffffffffu, fm[0], ho / COLS);
+      if (COLS > 1) {
+        const float fl1 = __shfl_sync(0xffffffffu, fm[COLS - 1], hl / COLS), fi1 = __shfl_sync(0xffffffffu, fm[COLS - 1], ho / COLS);
+        if (hl & 1) fl = fl1;
+        if (ho & 1) fi = fi1;
       }
+      if (lane % L_LANES == 0) part_l[wid][hl] = l_run[0] * fl;
+      if (lane % LO_LANES < LOW) part_lo[wid][ho][my_group + io] = lo_all[0] * fi;
+    }
     float* po = reinterpret_cast<float*>(ring);
 #pragma unroll
     for (int x = 0; x < (GT > 4 ? 2 : 1); ++x) {
