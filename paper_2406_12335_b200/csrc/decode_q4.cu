@@ -21,17 +21,18 @@
 //     inputs: both as a high half and a remainder, 2^-22;
 //   * rows are stored so that the 8 or 16 bytes a lane takes hold the channels it needs in an MMA operand, of every group.
 // A unit is split over a thread-block cluster; the slots of a CTA over eight or sixteen warps, 32 at a time.
-//   * An item of K or of V is 32 consecutive rows, two bulk copies (codes, parameters) into the warp's ring in shared memory.  As many
-//     as the ring holds are requested before the launch ahead has finished; the one row that it may have appended since (last_slot) is
-//     patched in.
+//   * An item of K or of V is 32 consecutive rows, two bulk copies (codes, parameters) into the warp's ring in shared memory.  Those
+//     of K, as many as the ring holds, are requested before the launch ahead has finished (after it: 256 units x 1639 slots 16.9 -> 17.9 us);
+//     the one row that it may have appended since (last_slot) is patched in.  The first of V go out while q and the state words are under
+//     way: what stands before the wait delays the CTAs that start last, when others of the launch ahead have just left their SMs.
 //   * A warp keeps its own softmax: its maximum, sum and partial output, without a barrier between the two products.
 //   * One more warp takes the incoming token, which is no part of any item: it quantises and stores the rows and is a partial of its own.
 //   * The CTA joins its partials, the cluster those of its CTAs by st.async into the partners' shared memory; every CTA then updates the
 //     indicators of its own slots, and every warp sends its eviction candidate to rank 0.
 // What bounds it (one head, d 128): instructions and their latency, not memory.  An item's two products are 645 instructions of a warp
-// (110 of them requests) for 5 KB, and a step has some 1000 more per warp that do not depend on its length.  32 units x 2049 slots: 6.7 us
-// per step in a chain of steps, of which the launch takes 1.2, preparing q 0.75, two items' K 0.85, V 1.3, joining partials, CTAs and candidates 1.9;
-// 256 units x 1639: 18.3 us, 4.0 TB/s.  Not faster: a warp that requests all rings' items; three CTAs an SM (72 registers spill); p sc of the next
+// (110 of them requests) for 5 KB, and a step has some 1000 more per warp that do not depend on its length.  32 units x 2049 slots: 6.2 us
+// per step in a chain of steps, of which the time between launches takes 0.7, q 0.85, two items' K 0.8, V 1.25, joining partials, CTAs and candidates
+// 2.6; 256 units x 1639: 16.9 us, 4.4 TB/s.  Not faster: a warp that requests all rings' items; three CTAs an SM (72 registers spill); p sc of the next
 // item formed while this one's products run (spills with eight warps in pairs: 18.7 -> 21.5 us; without spills 6.74 -> 6.97).
 #include <cooperative_groups.h>
 #include <cuda_fp16.h>
@@ -322,11 +323,11 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
     bulk_load(dst + Q4_ROWS * CODES, (is_v ? vp : kp) + (uint64_t)r0 * PARAMS, rows * PARAMS, bar);
   };
   const int n_alloc = wid < WARPS ? items_in(rows_alloc) : 0, early = min(depth, n_alloc), ahead = min(depth, 2 * n_alloc);
-  if (lane == 0)
+  if (elected())
     for (int j = 0; j < early; ++j) request(j, n_alloc, j);
   __syncwarp();
 
-  // Nothing but K and V rows is read before the previous launch has completed.
+  // Nothing but K rows is read before the previous launch has completed.
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int len_m = c.state.len[u], fs_m = c.state.free_slot[u], t = c.state.next_pos[u], ls = c.state.last_slot[u];
   // q for the B operand of K q^T, requested along with the words above.  Lane (n = r8, t4): channels 8 t4 .. 8 t4 + 7 of groups of its column.
@@ -338,7 +339,7 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
 #pragma unroll
     for (int g = 0; g < QG; ++g) q_raw[g].load(qp + (INT ? 64 : 32) * g);
     // the ring's first items of V, while these loads are under way
-    if (lane == 0)
+    if (elected())
       for (int j = early; j < ahead; ++j) request(j, n_alloc, j);
     __syncwarp();
   }
