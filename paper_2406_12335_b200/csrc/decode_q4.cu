@@ -235,7 +235,7 @@ __device__ __forceinline__ unsigned long long min_key(unsigned long long key) {
 // GT: 1 - one query head per cache; 4 - two to four, the columns of the second product are the heads' high halves and then the
 // remainders; 8 - five to eight, a column a head and two products.
 // Dynamic shared memory: rings [WARPS][depth][item], which take the warps' partial outputs in the end | the last partial [G][HD] |
-// logits [G][ld].
+// slices received [2 G HD at most] | logits [G][ld].
 template <int HD> constexpr int q4_item = Q4_ROWS * (HD / 2 + HD / 8);      // bytes of an item: codes, then parameters
 
 // ALONE: one CTA on an SM (eight warps then have 140 registers instead of 96: 32 units x 2049 slots 7.3 -> 6.8 us).
