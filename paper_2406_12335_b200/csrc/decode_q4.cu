@@ -11,14 +11,16 @@
 //     byte * q_lo + upper half / 16 * (q_hi - 16 q_lo), each factor as four signed digits of 8 bits in columns of their own, two groups
 //     side by side.  p_i sc_ig is an integer below 2^29 in four unsigned digits.  All products are exact; a fp32 q loses 2^-25 of the
 //     largest, p sc 2^-29 of the warp's largest;
-//   * several heads (m16n8k16 in fp16, 32-bit sums; a column or two for each head): a code in the low bits of a 16-bit word IS the fp16
-//     number code * 2^-24 (subnormal), one in bits 4-7 is code * 2^-20: unpacking is one AND per two codes and one shift per eight;
-//     the constant factors go into the other operand and the result.  The tensor cores align such a product by its nominal
-//     exponent of -14 and cut off what lies 24 bits below: 4e-5 of an output of four heads x 2001 slots, which 16 bits do not show.
-//     With fp32 inputs all codes are brought to bits 6-9 (code * 2^-18, a shift each).  The other operand's magnitude does not matter:
-//     q is scaled by a power of two per head, p_i sc_ig by one per warp and head that the largest of them determines.  bf16 inputs: q is exact
-//     in fp16, p_i sc_ig is rounded to its 11 bits (2^-12 of a term, an eighth of what the output's own rounding may be off by); fp32
-//     inputs: both as a high half and a remainder, 2^-22;
+//   * several heads (m16n8k16 in fp16, 32-bit sums; two columns for each head): a code in bits 6-9 of a 16-bit word IS the fp16 number
+//     code * 2^-18 (subnormal): unpacking is a shift and an AND per two codes; the constant factor goes into the result.  The tensor
+//     cores align such a product by its nominal exponent of -14 and cut off what lies 24 bits below the largest of a sum, hence not
+//     bits 0-3 and 4-7, where an AND alone would do: beside a channel of q that is 125 times the others logits were then off by 1.1e-5 to
+//     1.5e-5, so by 3e-6.
+//     The other operand's magnitude does not matter: q is scaled by a power of two per head, p_i sc_ig by one per warp and head that the
+//     largest of them determines.  p_i sc_ig and a q of 32 bits are a high half and a remainder, 2^-22 (with p_i sc_ig in one fp16, 2^-12,
+//     one bf16 output in six came out a step away from the nearest; now one in fifty at most.  Both together cost 5 to 10 %: 16 units x 4002
+//     slots, four heads, 9.6 -> 10.3 us per step; 128 x 2049, eight heads, 29.5 -> 32.5); a bf16 q fits one fp16 down to
+//     2^-28 of the head's largest channel, below that it is off by 2^-38 of that channel at most;
 //   * rows are stored so that the 8 or 16 bytes a lane takes hold the channels it needs in an MMA operand, of every group.
 // A unit is split over a thread-block cluster; the slots of a CTA over eight or sixteen warps, 32 at a time.
 //   * An item of K or of V is 32 consecutive rows, two bulk copies (codes, parameters) into the warp's ring in shared memory.  Those
@@ -248,17 +250,16 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
   constexpr bool INT = GT == 1;                                 // products in integers (see the top)
   constexpr int KP = INT ? NG / 2 : NG;                         // parameter words of a lane per K row
   constexpr int CODES = HD / 2, PARAMS = NG * 4, ITEM = q4_item<HD>;      // bytes of a row's codes and parameters, of an item
-  constexpr bool SPLIT = sizeof(T) == 4;                        // q and p sc have remainders beyond their high halves
-  constexpr int XC = GT > 4 && SPLIT ? 16 : 8;                  // columns of the second product's operand: see x_col
+  constexpr bool Q_REST = sizeof(T) == 4;                       // q has a remainder beyond its high half
+  constexpr int XC = GT > 4 ? 16 : 8;                           // columns of the second product's operand: see x_col
   constexpr int N = GT > 4 ? 1 : 2;                             // tiles a warp works on at a time (with eight heads: registers)
   constexpr int PG = N == 2 ? NG : VW;                          // groups of a lane where p sc is formed: a slot or half of one
   constexpr int XS = INT ? NG * 4 * 2 * Q4_TILE : N * NG * XC * Q4_TILE * 2;      // bytes of a warp's second operand
-  // where a product takes the four codes of a 16-bit word: in place, then 8 bits down (SPLIT: each in bits 6-9)
-  constexpr int CODE_EXP = SPLIT ? 18 : 24;                     // a code in an even channel stands for code * 2^-CODE_EXP
-  auto codes0 = [](uint32_t x) { return SPLIT ? x << 6 & 0x03c003c0u : x & 0x000f000fu; };
-  auto codes1 = [](uint32_t x) { return SPLIT ? x << 2 & 0x03c003c0u : x & 0x00f000f0u; };
-  auto codes2 = [](uint32_t x) { return SPLIT ? x >> 2 & 0x03c003c0u : x >> 8 & 0x000f000fu; };
-  auto codes3 = [](uint32_t x) { return SPLIT ? x >> 6 & 0x03c003c0u : x >> 8 & 0x00f000f0u; };
+  constexpr int CODE_EXP = 18;                                  // a code in bits 6-9 stands for code * 2^-CODE_EXP
+  auto codes0 = [](uint32_t x) { return x << 6 & 0x03c003c0u; };      // the four codes of a 16-bit word
+  auto codes1 = [](uint32_t x) { return x << 2 & 0x03c003c0u; };
+  auto codes2 = [](uint32_t x) { return x >> 2 & 0x03c003c0u; };
+  auto codes3 = [](uint32_t x) { return x >> 6 & 0x03c003c0u; };
   const int G = GT == 1 ? 1 : G_arg;
   // high half and remainder of head h: neighbours, i.e. in one lane's accumulators, or eight columns apart (two products)
   auto x_col = [](int h, int low) { return GT > 4 ? h + 8 * low : 2 * h + low; };
@@ -486,7 +487,7 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
     }
 
     // ---- B operand of K q^T
-    uint32_t qb[NG][INT ? 2 : 4], qr[GT > 1 && SPLIT ? NG : 1][4];
+    uint32_t qb[NG][INT ? 2 : 4], qr[GT > 1 && Q_REST ? NG : 1][4];
     // what a sum is to be multiplied by (INT: of the lane's two digits); sums of q over groups, * scale
     float q_back[2], qsum[INT ? NG / 2 : NG][2];
     {
@@ -545,10 +546,10 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
         for (int g = 0; g < NG; ++g)
 #pragma unroll
           for (int x = 0; x < 4; ++x) {
-            const float f = x & 1 && !SPLIT ? up * 0.0625f : up, p0 = q[g][x] * f, p1 = q[g][x + 4] * f;      // (odd channels' codes stand four bits higher)
+            const float p0 = q[g][x] * up, p1 = q[g][x + 4] * up;
             const __half2 h = __floats2half2_rn(p0, p1);
             qb[g][x] = *reinterpret_cast<const uint32_t*>(&h);
-            if constexpr (SPLIT) qr[g][x] = half2_of(p0 - __low2float(h), p1 - __high2float(h));
+            if constexpr (Q_REST) qr[g][x] = half2_of(p0 - __low2float(h), p1 - __high2float(h));
           }
         // (an accumulator's columns are heads 2 t4 and 2 t4 + 1; their sums are with the lanes of those columns)
 #pragma unroll
@@ -663,7 +664,7 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
             d[0] = d[1] = d[2] = d[3] = 0.f;
             mma_f16(d, codes0(xa), codes0(xb), codes1(xa), codes1(xb), qb[g][0], qb[g][1]);
             mma_f16(d, codes2(xa), codes2(xb), codes3(xa), codes3(xb), qb[g][2], qb[g][3]);
-            if constexpr (SPLIT) {
+            if constexpr (Q_REST) {
               mma_f16(d, codes0(xa), codes0(xb), codes1(xa), codes1(xb), qr[g][0], qr[g][1]);
               mma_f16(d, codes2(xa), codes2(xb), codes3(xa), codes3(xb), qr[g][2], qr[g][3]);
             }
@@ -826,12 +827,10 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
               uint16_t* to = reinterpret_cast<uint16_t*>(xs[wid]) + ((my_group + i) * XC + x_col(h, 0)) * Q4_TILE + x_at;
               to[0] = __half_as_ushort(__low2half(hh));
               if (PG > 1) to[XC * Q4_TILE] = __half_as_ushort(__high2half(hh));
-              if constexpr (SPLIT) {
-                const __half2 hl = __floats2half2_rn(x0 - __low2float(hh), x1 - __high2float(hh));
-                to += (x_col(h, 1) - x_col(h, 0)) * Q4_TILE;
-                to[0] = __half_as_ushort(__low2half(hl));
-                if (PG > 1) to[XC * Q4_TILE] = __half_as_ushort(__high2half(hl));
-              }
+              const __half2 hl = __floats2half2_rn(x0 - __low2float(hh), x1 - __high2float(hh));
+              to += (x_col(h, 1) - x_col(h, 0)) * Q4_TILE;
+              to[0] = __half_as_ushort(__low2half(hl));
+              if (PG > 1) to[XC * Q4_TILE] = __half_as_ushort(__high2half(hl));
             }
           }
         }
@@ -871,7 +870,7 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
             const uint32_t xa = __byte_perm(vw[a][0][g >> 1], vw[a][1][g >> 1], sel), xb = __byte_perm(vw[a][2][g >> 1], vw[a][3][g >> 1], sel);
             mma_f16(o_acc[g][0], codes0(xa), codes1(xa), codes0(xb), codes1(xb), b.x, b.y);
             mma_f16(o_acc[g][1], codes2(xa), codes3(xa), codes2(xb), codes3(xb), b.x, b.y);
-            if constexpr (GT > 4 && SPLIT) {
+            if constexpr (GT > 4) {
               const uint2 d = *reinterpret_cast<const uint2*>(xh + 8 * Q4_TILE);
               mma_f16(o_acc[g][0], codes0(xa), codes1(xa), codes0(xb), codes1(xb), d.x, d.y);
               mma_f16(o_acc[g][1], codes2(xa), codes3(xa), codes2(xb), codes3(xb), d.x, d.y);
@@ -890,8 +889,8 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
       for (int a = 0; a < 2; a += N) v_rows(j, a);
     }
     fetch(tid);
-    // ---- the warp's partial, relative to the CTA's maximum: sums of p (even lanes) and of p lo, and O^T with its constant factors
-    // (codes in odd channels stand four bits higher), into the ring
+    // ---- the warp's partial, relative to the CTA's maximum: sums of p (even lanes) and of p lo, and O^T with its constant factor,
+    // into the ring
     if (!bad && !bar_wait(s32(&k_done), 0)) bad = true;
     __syncwarp();
     constexpr int COLS = GT > 4 ? 2 : 1;     // heads of this lane's columns of the accumulators: 2 t4 + x or t4
@@ -944,7 +943,7 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
             o[i] *= fo[0];
           } else {                           // the remainder's column beside the head's
             o[i] = GT > 4 ? o_acc[g][i >> 1][2 * (i & 1) + x] : o_acc[g][i >> 1][2 * (i & 1)] + o_acc[g][i >> 1][2 * (i & 1) + 1];
-            o[i] *= i & 1 && !SPLIT ? fo[x] * 0.0625f : fo[x];
+            o[i] *= fo[x];
           }
         }
         if (h < G) *reinterpret_cast<float4*>(po + h * HD + 32 * g + 4 * r8) = make_float4(o[0], o[1], o[2], o[3]);

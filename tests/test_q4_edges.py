@@ -1,0 +1,76 @@
+"""The 4-bit decode state at its edges on the GPU: precision where a sum's terms differ much, magnitudes at the ends of the range, values
+that are not finite, wide batches of copies.  Tolerances count roundings; the reference is tests/q4_reference.py, in 64 bits."""
+import pytest
+import torch
+
+from tests import parity as P
+from tests import q4_reference as Q
+from tests.test_q4 import DT, _equal, _filled, _gen, _params, _rows, _status
+
+pytestmark = pytest.mark.gpu
+
+
+def _packed(p, k, v):
+    """A full 4-bit state of the rows k, v [units, B, d]."""
+    V = P.vatp()
+    wide, c = _filled(p, p.budget, form="wide"), V.CacheQ4(p)
+    wide.k_cache[0, :, :p.budget], wide.v_cache[0, :, :p.budget] = k.to(wide.k_cache.dtype), v.to(wide.k_cache.dtype)
+    V.vatp_cache_pack_q4(p, wide, c)
+    torch.cuda.synchronize()
+    return c
+
+
+def _reference(c, p):
+    return Q.State(c, p.head_dim, p.budget, p.n_sink, p.n_recent, p.scale)
+
+
+# ------------------------------------------------------------------------------------------------ precision
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("G", [1, 2, 4, 8])
+def test_products_of_probabilities_and_scales_keep_32_bits(dtype, G):
+    """All rows of V the same, all probabilities but one in 32 the same: what rounding p sc does to a term does not average out, and the
+    outputs are differences of large terms."""
+    V, units, B, d = P.vatp(), 16, 255, 64
+    p = _params(dtype, 1, units * G, units if G > 1 else 0, d, B=B)
+    k = torch.zeros(units, B, d, device="cuda")
+    k[..., 0] = 0.3
+    k[:, ::32, 0] = torch.linspace(1.0, 2.0, units, device="cuda")[:, None]        # a warp's 32 rows: one with a larger logit
+    v = (torch.arange(d, device="cuda") % 16 - 8.0).expand(units, B, d)            # lo -8, sc 1: code 8 stands for 0
+    c = _packed(p, k, v)
+    q = torch.zeros(1, units * G, d, device="cuda", dtype=DT[dtype])
+    q[0, :, 0] = torch.linspace(2.0, 5.0, units * G, device="cuda").to(q.dtype)    # (logits 0.2 to 1.1 apart, none of them 0)
+    k1, v1, out = torch.zeros(1, units, d, device="cuda", dtype=q.dtype), v[:, 0][None].to(q.dtype).contiguous(), torch.empty_like(q)
+    want, _, _, _, rel, v_mag = _reference(c, p).step(q.view(units, G, d), k1.view(units, d), v1.view(units, d))
+    V.vatp_decode_step_q4(p, c, q, k1, v1, out)
+    torch.cuda.synchronize()
+    off = (out.double().view(want.shape) - want).abs()
+    # rel: what a probability may be off by; 2^-20: p sc in two halves and the sums of 256 terms in 32 bits; half a step of the output.
+    # (With one fp16 for p sc: 11 to 15 times the bound.)
+    bound = (rel[..., None] + 2.0 ** -20) * v_mag + torch.finfo(q.dtype).eps / 2 * want.abs()
+    assert torch.all(off <= bound), float((off / bound).max())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("G", [1, 2, 4, 8])
+def test_logits_beside_a_channel_of_large_queries(dtype, G):
+    """A channel of q is 125 times the others, and the keys are nearly constant in it: the other channels decide."""
+    V, units, B, d = P.vatp(), 4, 1500, 128
+    p = _params(dtype, 1, units * G, units if G > 1 else 0, d, B=B)
+    g = _gen(31)
+    k, v = (torch.randn(units, B, d, generator=g, device="cuda").clamp(-2.9, 2.9) for _ in range(2))
+    k[..., 0] = 3.0                                                                # the largest of its group
+    c = _packed(p, k, v)
+    c.acc.zero_()
+    q = torch.randn(1, units * G, d, generator=g, device="cuda").to(DT[dtype])
+    q[..., 0] = 125.0
+    k1, v1 = (torch.randn(1, units, d, generator=g, device="cuda").clamp(-2.9, 2.9).to(q.dtype) for _ in range(2))
+    k1[..., 0] = 3.0
+    _, pm, _, _, _, _ = _reference(c, p).step(q.view(units, G, d), k1.view(units, d), v1.view(units, d))
+    V.vatp_decode_step_q4(p, c, q, k1, v1, torch.empty_like(q))
+    torch.cuda.synchronize()
+    got = c.acc.double().view(units, -1)
+    # A sum of products on the tensor cores cuts its terms off 2^-24 below the largest one's nominal magnitude, 2^-14 q where a code counts
+    # 2^-18: 2^-20 * 125 * sc * scale = 4.2e-6 of a logit (sc 0.4, scale 128^-1/2) a term.  34 such errors in the group of that channel, even
+    # between 0 and that: 7e-6 rms.  Logits of 33 in natural units, 48 in powers of two, have an ulp of 3.8e-6; eight roundings: 4e-6 rms.
+    # Together 8e-6, over 6000 slots to a few percent.  (Codes that count 2^-24 were seen to lose 1.1e-5 to 1.5e-5.)
+    assert (got - pm).norm() <= 9.7e-6 * pm.norm(), float((got - pm).norm() / pm.norm())
