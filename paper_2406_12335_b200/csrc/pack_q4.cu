@@ -135,6 +135,7 @@ pack_q4_kernel(const __grid_constant__ CopyPlan plan, Shape sh, int B, int cap, 
       *reinterpret_cast<uint16_t*>(row + q4_byte<HD>(g, j)) = (uint16_t)q4_codes(q, x[t].at(4 * j), x[t].at(4 * j + 1), x[t].at(4 * j + 2), x[t].at(4 * j + 3));
   }
   const uint32_t rows = __ballot_sync(0xffffffffu, src >= 0 && g == 0);           // bit NG * r: row r is live
+  __syncwarp();                                                   // (a vote orders no memory)
   const int at = lane * 16, r = at / (HD / 2);
   if (rows >> (NG * r) & 1u) {
 #pragma unroll

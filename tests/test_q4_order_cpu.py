@@ -1,0 +1,17 @@
+"""Order that the kernels of the 4-bit state need and that no result shows on one chip: read from their source."""
+import re
+
+from tests.test_dependent_launches_cpu import _code, _dependent_kernels
+
+
+def _body(name, kernel):
+    return {k: body for k, _, body in _dependent_kernels(_code(name))}[kernel]
+
+
+def test_codes_pass_through_shared_memory_behind_a_barrier_of_the_warp():
+    """A vote exchanges values and orders no memory."""
+    body = _body("pack_q4.cu", "pack_q4_kernel")
+    stores = [m.start() for m in re.finditer(r"\*reinterpret_cast<uint16_t\*>\(row \+", body)]
+    loads = [m.start() for m in re.finditer(r"\*reinterpret_cast<const uint4\*>\(stage", body)]
+    assert stores and loads and "unsigned char* row = stage[wid][t]" in body
+    assert "__syncwarp();" in body[stores[-1]:loads[0]]
