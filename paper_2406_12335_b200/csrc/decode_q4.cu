@@ -412,7 +412,6 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
       if (lane == 0) {
         new_norm_s = nv;
         c.state.vnorm[base + fs_local] = nv;
-        c.state.pos[base + fs_local] = t;
       }
     }
     for (int row = rows_alloc; row < cnt; ++row) {
@@ -1071,12 +1070,14 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
         out_slot = best.slot;
         ev = best.pos;
         left = hi - 1;
-        if (write && VATP_INB(out_slot, cap, dev_status)) c.state.pos[(int64_t)u * cap + out_slot] = -1;
       } else {                             // nothing eligible (cannot happen when F + R <= B): keep the state consistent
         out_slot = min(hi, cap - 1);
       }
     }
     if (write) {
+      // (both positions by one thread, in this order: they are the same word where the incoming token goes at once)
+      if (fs < hi) c.state.pos[(int64_t)u * cap + fs] = t;
+      if (left < hi && VATP_INB(out_slot, cap, dev_status)) c.state.pos[(int64_t)u * cap + out_slot] = -1;
       c.state.len[u] = left;
       c.state.free_slot[u] = out_slot;
       c.state.next_pos[u] = t + 1;

@@ -15,3 +15,15 @@ def test_codes_pass_through_shared_memory_behind_a_barrier_of_the_warp():
     loads = [m.start() for m in re.finditer(r"\*reinterpret_cast<const uint4\*>\(stage", body)]
     assert stores and loads and "unsigned char* row = stage[wid][t]" in body
     assert "__syncwarp();" in body[stores[-1]:loads[0]]
+
+
+def _pos_stores(body, state):
+    return [m.start() for m in re.finditer(re.escape(state) + r"pos\[[^;=]*\] = ", body)]
+
+
+def test_positions_of_a_step_are_written_by_one_thread():
+    """The incoming token's position and the release of a slot may meet in the same word (the incoming token goes at once)."""
+    body = _body("decode_q4.cu", "decode_q4_kernel")
+    last = body.index("else if (rank == 0) {")
+    at = _pos_stores(body, "c.state.")
+    assert at and all(x > last for x in at) and "if (write) {" in body[last:at[0]]
