@@ -524,10 +524,7 @@ decode_mma_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
       if (wid == new_warp) {
         __nv_bfloat16* dst = (__nv_bfloat16*)(lane < 16 ? c.k_cache : c.v_cache) + ((int64_t)u * cap + fs) * HD;
         if (has_chunk) reinterpret_cast<uint4*>(dst)[lane & 15] = new_raw;
-        if (lane == 0) {
-          c.vnorm[(int64_t)u * cap + fs] = new_norm;
-          c.pos[(int64_t)u * cap + fs] = t;
-        }
+        if (lane == 0) c.vnorm[(int64_t)u * cap + fs] = new_norm;
       }
     }
   };
@@ -960,11 +957,13 @@ decode_mma_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
         out_slot = best_slot;
         ev = best_pos;
         left = hi - 1;
-        if (VATP_INB(out_slot, cap, dev_status)) c.pos[(int64_t)u * cap + out_slot] = -1;
       } else {   // nothing eligible (cannot happen when F + R <= B): keep the state consistent
         out_slot = min(hi, cap - 1);
       }
     }
+    // (both positions by one thread, in this order: they are the same word where the incoming token goes at once)
+    if (fs >= 0 && fs < hi) c.pos[(int64_t)u * cap + fs] = t;
+    if (left < hi && VATP_INB(out_slot, cap, dev_status)) c.pos[(int64_t)u * cap + out_slot] = -1;
     c.len[u] = left;
     c.free_slot[u] = out_slot;
     c.next_pos[u] = t + 1;

@@ -27,3 +27,10 @@ def test_positions_of_a_step_are_written_by_one_thread():
     last = body.index("else if (rank == 0) {")
     at = _pos_stores(body, "c.state.")
     assert at and all(x > last for x in at) and "if (write) {" in body[last:at[0]]
+
+
+def test_positions_of_a_16_bit_step_are_written_by_one_thread():
+    body = _body("decode_mma.cu", "decode_mma_kernel")
+    last = body.rindex("if (rank == 0 && tid == 0) {")
+    at = _pos_stores(body, "c.")
+    assert at and all(x > last for x in at)
