@@ -136,12 +136,18 @@ def vatp_workspace_bytes(p: Params) -> int:
     return int(lib.vatp_workspace_bytes(C.byref(p)))
 
 
+def _shape(p: Params):
+    """What the arrays of a decode state depend on, its batch and budget first and the type of 16- and 32-bit rows last."""
+    return p.batch, p.budget, p.kv_heads or p.heads, p.head_dim, p.window_w if p.indicator == IND_WINDOW else 0, p.dtype
+
+
 class _State:
     """The per-slot and per-unit arrays that both forms of the decode state have."""
 
     def __init__(self, p: Params, device, share):
         b, h, cap = p.batch, (p.kv_heads or p.heads), int(lib.vatp_cache_capacity(p.budget))
         self.cap, self.budget, self.batch = cap, p.budget, b
+        self.made_for = _shape(p)
         if share is not None:
             if (share.cap, share.budget, share.pos.shape[:2]) != (cap, p.budget, (b, h)) or (share.ring is not None) != (p.indicator == IND_WINDOW) \
                     or (share.ring is not None and share.ring.shape[2] != p.window_w):
@@ -289,9 +295,15 @@ def vatp_decode_step_q4(p: Params, cache: CacheQ4, q_new, k_new, v_new, out, *, 
 
 def vatp_cache_copy(p: Params, src, dst, src_of, *, dev_status=None, stream=None):
     """Entry b of `dst` (which p describes) becomes entry src_of[b] of `src`; SEQ_KEEP leaves it, SEQ_FREE empties it.  src_of: int32
-    [p.batch] on the device; both states Cache (vatp_cache_copy) or both CacheQ4 (vatp_cache_copy_q4)."""
+    [p.batch] on the device; both states Cache (vatp_cache_copy) or both CacheQ4 (vatp_cache_copy_q4).  A map of another type, length
+    or device and states that do not fit p or one another are a ValueError."""
     if type(src) is not type(dst):
         raise TypeError("both states must hold their rows in the same form")
+    n = -1 if isinstance(dst, CacheQ4) else None                   # (4-bit rows: whatever type they came from)
+    if dst.made_for[:n] != _shape(p)[:n] or src.made_for[2:n] != dst.made_for[2:n]:
+        raise ValueError("a state of other parameters")
+    if src_of is not None and (src_of.dtype != torch.int32 or src_of.shape != (p.batch,) or not src_of.is_contiguous() or src_of.device != dst.pos.device):
+        raise ValueError("src_of: int32, one for each entry of dst, contiguous, where dst is")
     name = "vatp_cache_copy_q4" if isinstance(dst, CacheQ4) else "vatp_cache_copy"
     _check(getattr(lib, name)(C.byref(p), C.byref(src.struct), src.batch, src.budget, C.byref(dst.struct), _ptr(src_of), _ptr(dev_status),
                               _stream(stream)), name)
