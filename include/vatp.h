@@ -126,6 +126,8 @@ typedef struct {
  *   code = rint((x - lo) * (1 / sc)), ties to even, at most 15;    0 where sc = 0
  * with the difference, the quotients and the product each rounded to fp32, and stands for lo + code * sc.  No value is clamped,
  * and |x - (lo + code * sc)| <= sc / 2 up to fp32 rounding.  Values (of queries too) are assumed below 2^100 in magnitude.
+ * A group with a NaN or an infinity among its values is stored as sc = lo = NaN, its codes without meaning, and stands for NaN
+ * in all its channels.
  * Channel 32 g + 4 j + e (j < 8, e < 4) is a nibble of byte j * (head_dim / 16) + 2 g + e / 2 of the row, the low nibble for an
  * even e: sixteen bytes in a row hold the same channels of all groups, which is how the generation step reads them.
  * With head_dim 128 a row takes 64 + 16 bytes (256 in bf16).

@@ -43,11 +43,11 @@ template <> struct Group32<__nv_bfloat16> {
 #pragma unroll
     for (int i = 1; i < 16; ++i) {
       const __nv_bfloat162 x = reinterpret_cast<const __nv_bfloat162&>(w[i]);
-      a = __hmin2(a, x);
-      b = __hmax2(b, x);
+      a = __hmin2_nan(a, x);
+      b = __hmax2_nan(b, x);
     }
-    mn = fminf(__low2float(a), __high2float(a));
-    mx = fmaxf(__low2float(b), __high2float(b));
+    mn = min_nan(__low2float(a), __high2float(a));
+    mx = max_nan(__low2float(b), __high2float(b));
   }
 };
 template <> struct Group32<float> {
@@ -67,7 +67,7 @@ template <> struct Group32<float> {
   __device__ __forceinline__ void range(float& mn, float& mx) const {
     mn = mx = x[0];
 #pragma unroll
-    for (int i = 1; i < 32; ++i) { mn = fminf(mn, x[i]); mx = fmaxf(mx, x[i]); }
+    for (int i = 1; i < 32; ++i) { mn = min_nan(mn, x[i]); mx = max_nan(mx, x[i]); }
   }
 };
 

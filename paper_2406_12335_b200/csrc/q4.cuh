@@ -9,14 +9,27 @@ constexpr float Q4_LEAST = 7.888609052210118e-31f;     // 2^-100: a smaller scal
 
 // scale, low end and reciprocal of a group whose values span [mn, mx].  The low end is rounded down and the scale up, so that no
 // value lies outside [lo, lo + 15 sc] and the nearest code is off by half a step at most.
+// A group with a value that is not finite, or with a range beyond that of fp32, stands for NaN: both parameters are, whatever the codes.
 struct Q4Group {
   float sc, lo, inv;
 };
+// (of a NaN and a number: NaN)
+__device__ __forceinline__ float min_nan(float a, float b) {
+  float x;
+  asm("min.NaN.f32 %0, %1, %2;" : "=f"(x) : "f"(a), "f"(b));
+  return x;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float x;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(x) : "f"(a), "f"(b));
+  return x;
+}
 __device__ __forceinline__ Q4Group q4_group(float mn, float mx) {
   Q4Group g;
   g.lo = __bfloat162float(__float2bfloat16_rd(mn));
   g.sc = __bfloat162float(__float2bfloat16_ru(__fdiv_rn(__fsub_rn(mx, g.lo), 15.f)));
   if (g.sc < Q4_LEAST) g.sc = 0.f;
+  if (!(g.sc < INFINITY)) g.sc = g.lo = __uint_as_float(0x7fff0000u);
   g.inv = g.sc > 0.f ? __frcp_rn(g.sc) : 0.f;
   return g;
 }
@@ -42,11 +55,11 @@ template <int HD> __host__ __device__ constexpr int q4_byte(int g, int j) { retu
 // One row by one warp: lane l < HD / 4 has channels 4 l .. 4 l + 3 (group l / 8, j = l mod 8) in x.  Returns the two code bytes
 // and sets `params` of the lane's group; lanes from HD / 4 on take part in the exchange only.
 __device__ __forceinline__ uint32_t q4_row(const float (&x)[4], uint32_t& params) {
-  float mn = fminf(fminf(x[0], x[1]), fminf(x[2], x[3])), mx = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
+  float mn = min_nan(min_nan(x[0], x[1]), min_nan(x[2], x[3])), mx = max_nan(max_nan(x[0], x[1]), max_nan(x[2], x[3]));
 #pragma unroll
   for (int o = 1; o < 8; o <<= 1) {
-    mn = fminf(mn, __shfl_xor_sync(0xffffffffu, mn, o));
-    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+    mn = min_nan(mn, __shfl_xor_sync(0xffffffffu, mn, o));
+    mx = max_nan(mx, __shfl_xor_sync(0xffffffffu, mx, o));
   }
   const Q4Group g = q4_group(mn, mx);
   params = q4_params(g);

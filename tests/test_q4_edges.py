@@ -5,7 +5,7 @@ import torch
 
 from tests import parity as P
 from tests import q4_reference as Q
-from tests.test_q4 import DT, _equal, _filled, _gen, _params, _rows, _status
+from tests.test_q4 import DT, _filled, _gen, _params, _rows, _status
 
 pytestmark = pytest.mark.gpu
 
@@ -74,3 +74,38 @@ def test_logits_beside_a_channel_of_large_queries(dtype, G):
     # between 0 and that: 7e-6 rms.  Logits of 33 in natural units, 48 in powers of two, have an ulp of 3.8e-6; eight roundings: 4e-6 rms.
     # Together 8e-6, over 6000 slots to a few percent.  (Codes that count 2^-24 were seen to lose 1.1e-5 to 1.5e-5.)
     assert (got - pm).norm() <= 9.7e-6 * pm.norm(), float((got - pm).norm() / pm.norm())
+
+
+# ------------------------------------------------------------------------------------------------ values that are not finite
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f32", 64)])
+def test_groups_that_are_not_finite_are_stored_as_nan(dtype, d, bad):
+    """By compaction, conversion and the step: the group is NaN, its neighbours are what they were."""
+    V, B, h = P.vatp(), 40, 3
+    p, g = _params(dtype, 1, h, 0, d, T=B, B=B), _gen(12)
+    k, v = (_rows(g, 1, h, B, d, dtype=dtype) for _ in range(2))
+    group = torch.zeros(1, h, B, d // 32, dtype=torch.bool, device="cuda")
+    for row, at in ((0, 0), (7, 33), (20, 31), (39, d - 1)):                       # row 20: every head's whole group
+        k[:, 1, row, at], group[:, 1, row, at // 32] = bad, True
+    k[:, :, 20, :32], group[:, :, 20, 0] = bad, True
+    want = Q.stored(torch.where(group.repeat_interleave(32, -1), torch.zeros_like(k), k)).float().to(k.dtype)
+    want.masked_fill_(group.repeat_interleave(32, -1), float("nan"))
+    kept = torch.arange(B, dtype=torch.int32, device="cuda").expand(1, h, B).contiguous()
+    one = torch.ones(1, h, B, device="cuda")
+    wide, back = V.Cache(p), V.Cache(p)
+    V.vatp_compact(p, k, v, one, one, kept, wide)
+    for call in ("compact", "pack", "step"):
+        c = V.CacheQ4(p)
+        if call == "compact":
+            V.vatp_compact_q4(p, k, v, one, one, kept, c)
+        elif call == "pack":
+            V.vatp_cache_pack_q4(p, wide, c)
+        else:
+            for i in range(B):                                                     # into an empty cache, token by token
+                q = torch.zeros(1, h, d, dtype=k.dtype, device="cuda")
+                V.vatp_decode_step_q4(p, c, q, k[:, :, i].contiguous(), v[:, :, i].contiguous(), torch.empty_like(q))
+        V.vatp_cache_unpack_q4(p, c, back)
+        torch.cuda.synchronize()
+        assert torch.equal(torch.isnan(c.k_params[:, :, :B]), group[..., None].expand(-1, -1, -1, -1, 2)), call
+        torch.testing.assert_close(back.k_cache[:, :, :B], want, rtol=0, atol=0, equal_nan=True, msg=call)
+        assert torch.equal(back.v_cache[:, :, :B], Q.stored(v).float().to(v.dtype)), call
