@@ -344,7 +344,8 @@ vatp_status vatp_cache_unpack_q4(const vatp_params* params, const vatp_cache_q4*
 
 /*
  * vatp_decode_step on the 4-bit state.  The incoming row is quantised when it is stored and takes part as stored, like every other
- * row; its norm (Eq. 4) is that of k_new's and v_new's values as given.  Up to eight query heads per KV head
+ * row; its norm (Eq. 4) is that of k_new's and v_new's values as given.  A NaN in q_new or in a row that holds a token makes those
+ * outputs and indicators NaN that depend on it (with a history window the sums then mean nothing until it has left).  Up to eight query heads per KV head
  * (VATP_ERR_UNSUPPORTED beyond, and for budgets whose logits do not fit into the shared memory of the CTAs of a unit).
  * Everything else is as in vatp_decode_step, except that VATP_FLAG_DECODE_OVERLAP has no effect: every step waits for all earlier
  * work in the stream.

@@ -535,7 +535,8 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
           if (t4 & 1) qsum[g][0] = 0.f;
           qsum[g][1] = 0.f;
         }
-        const float back = __uint_as_float((uint32_t)(ex - 29 + 127) << 23) * scale_log2;
+        // (integers do not hold what is not finite: the logits become NaN)
+        const float back = most < INFINITY ? __uint_as_float((uint32_t)(ex - 29 + 127) << 23) * scale_log2 : __uint_as_float(0x7fff0000u);
         q_back[0] = t4 & 1 ? back * 65536.f : back;
         q_back[1] = q_back[0] * 256.f;
       } else {
@@ -808,8 +809,8 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
 #pragma unroll
       for (int h = 0; h < GT; ++h)
         if (GT == 1 || h < G) {
-          // (no live slot so far: m_own is -inf)
-          const float p = s[h] > -INFINITY ? exp2_fast(s[h] - m_own[h]) : 0.f, y = p * pow2((int)m_own[h] - (J[h] - 126 - X_TOP));
+          // (no live slot so far: m_own is -inf; a NaN stays one, and the sums with it)
+          const float p = s[h] == -INFINITY ? 0.f : exp2_fast(s[h] - m_own[h]), y = p * pow2((int)m_own[h] - (J[h] - 126 - X_TOP));
           l_run[h] += p;
 #pragma unroll
           for (int i = 0; i < PG; ++i) {

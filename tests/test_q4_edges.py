@@ -109,3 +109,42 @@ def test_groups_that_are_not_finite_are_stored_as_nan(dtype, d, bad):
         assert torch.equal(torch.isnan(c.k_params[:, :, :B]), group[..., None].expand(-1, -1, -1, -1, 2)), call
         torch.testing.assert_close(back.k_cache[:, :, :B], want, rtol=0, atol=0, equal_nan=True, msg=call)
         assert torch.equal(back.v_cache[:, :, :B], Q.stored(v).float().to(v.dtype)), call
+
+
+@pytest.mark.parametrize("where", ["k row", "v row", "k row of a warp's last slots", "q", "q inf", "k_new", "v_new"])
+@pytest.mark.parametrize("dtype,G,d,B", [("bf16", 1, 128, 700), ("f32", 1, 64, 150), ("bf16", 4, 128, 700), ("f32", 3, 64, 90), ("bf16", 8, 64, 400)])
+def test_a_nan_reaches_the_outputs(dtype, G, d, B, where):
+    """Where the formulas give NaN the step gives it; other units and heads are what they would be, and the state's words stay sound."""
+    V, units, bad = P.vatp(), 3, float("nan")
+    p, g = _params(dtype, 1, units * G, units if G > 1 else 0, d, B=B, F=2, R=3), _gen(13)
+    q, k, v = (_rows(g, 1, n, d, dtype=dtype) for n in (units * G, units, units))
+    clean, c = _filled(p, B), _filled(p, B)
+    q1, k1, v1 = q.clone(), k.clone(), v.clone()
+    head = 2 * G - 1                                                               # the last of unit 1
+    if "row" in where:
+        row = B - 1 if "last" in where else 40
+        (c.k_params if where[0] == "k" else c.v_params)[:, 1, row, 1] = bad
+    elif where[0] == "q":
+        q1[:, head, 5] = float("inf") if "inf" in where else bad
+    else:
+        (k1 if where[0] == "k" else v1)[:, 1, d - 1] = bad
+    want, pm, _, may_go, _, _ = Q.State(c, d, B, 2, 3, p.scale).step(q1.view(units, G, d), k1.view(units, d), v1.view(units, d))
+    got = []
+    for cache, a, b, e in ((clean, q, k, v), (c, q1, k1, v1)):
+        out, evicted, status = torch.empty_like(q), torch.empty(1, units, dtype=torch.int32, device="cuda"), _status()
+        V.vatp_decode_step_q4(p, cache, a, b, e, out, evicted_pos=evicted, dev_status=status)
+        torch.cuda.synchronize()
+        assert int(status) == 0
+        got.append(out.view(units, G, d))
+    assert torch.any(torch.isnan(want)) and torch.equal(torch.isnan(got[1]), torch.isnan(want))
+    same = ~torch.isnan(want).flatten(1).any(-1)
+    assert torch.equal(got[0][same], got[1][same]) and same.tolist() == [True, False, True]
+    if where[0] == "q":                                                            # the unit's other heads
+        assert torch.equal(got[0][1, :G - 1], got[1][1, :G - 1])
+    live, acc = c.pos.view(units, -1) >= 0, c.acc.view(units, -1)
+    assert torch.equal(torch.isnan(acc)[live], torch.isnan(pm)[live])
+    assert torch.equal(acc[[0, 2]], clean.acc.view(units, -1)[[0, 2]])
+    assert torch.all(c.len == B) and torch.all(live[:, :B + 1].sum(-1) == B)
+    slot = c.free_slot.view(-1).long()
+    u = torch.arange(units, device="cuda")
+    assert torch.all(may_go[u, slot]) and not torch.any(live[u, slot])
