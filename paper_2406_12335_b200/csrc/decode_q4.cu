@@ -55,6 +55,7 @@ constexpr int Q4_HEADS = 8;            // query heads of a unit at most (columns
 constexpr int Q4_EXTRA = 8;            // slots beyond the tiles that the last warp takes at most
 constexpr int Q4_DEPTH = 8;            // items in a warp's ring at most
 constexpr int Q4_FLUSH = 64 * Q4_ROWS;      // 255 * 15 * 257 * 2048 < 2^31
+constexpr int Q4_NO_J = -1000000;           // exponent of p sc before the first slot
 constexpr float Q4_LOG2E = 1.4426950408889634f;
 constexpr unsigned long long Q4_NO_KEY = ~0ull;
 
@@ -711,8 +712,8 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
     if (lane == 0) bar_arrive(s32(&k_done));
 
     // ---- O^T += V^T (p sc): A = codes (16 channels x 16 or 32 slots), B = p sc by slot and head, scaled by a power of two to fit fp16
-    // (2^(13 - J)) or 32-bit integers (2^(29 - J)).  J follows the largest s + log2 sc (rounded up) with a slack of 2^2; when it moves,
-    // what has been summed up is rescaled (a power of two).
+    // (2^(13 - J)) or 32-bit integers (2^(29 - J)).  J follows the largest log2 of p sc (rounded up; p relative to the warp's maximum) with
+    // a slack of 2^2; when it moves, what has been summed up is rescaled (a power of two).
     constexpr int X_TOP = INT ? 29 : 13;
     float o_acc[NG][2][4];                   // INT: [group][0]: channels 4 r8 .. + 3 of the group, of this lane's digits
     int o_int[INT ? NG : 1][2][4];           // sums over codes lo + 16 hi of a byte, and over 16 hi
@@ -723,15 +724,16 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
         o_acc[g][i][0] = o_acc[g][i][1] = o_acc[g][i][2] = o_acc[g][i][3] = 0.f;
         if (INT) o_int[g][i][0] = o_int[g][i][1] = o_int[g][i][2] = o_int[g][i][3] = 0;
       }
-    // this warp's maxima, rounded up to integers: p is taken relative to them, and what it is scaled by is a power of two (in one
-    // exponential with s, 2^29 p would have lost eight bits); of this lane's slots (and groups): sum of p, sum of p lo
+    // this warp's maxima, rounded up to integers (0 without a live slot): p is taken relative to them, and what it is scaled by is a power of two
+    // (in one exponential with s, 2^29 p would have lost eight bits); of this lane's slots (and groups): sum of p, sum of p lo
     float m_own[GT], l_run[GT], lo_run[GT][PG];
     int J[GT];
 #pragma unroll
     for (int h = 0; h < GT; ++h) {
-      m_own[h] = GT == 1 || h < G ? ceilf(fminf(part_m[wid][h], 1e9f)) : -INFINITY;
+      m_own[h] = GT == 1 || h < G ? ceilf(part_m[wid][h]) : 0.f;
+      if (m_own[h] == -INFINITY) m_own[h] = 0.f;
       l_run[h] = 0.f;
-      J[h] = -1000000000;
+      J[h] = Q4_NO_J;
 #pragma unroll
       for (int i = 0; i < PG; ++i) lo_run[h][i] = 0.f;
     }
@@ -767,7 +769,8 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
       for (int h = 0; h < GT; ++h) {
         f[h] = 1.f;
         if (GT == 1 || h < G) {
-          const int top = __reduce_max_sync(0xffffffffu, __float2int_ru(fminf(s[h], 1e9f)) + ev);      // (-inf: the least integer)
+          s[h] -= m_own[h];                  // log2 p: not above 0, -inf for a slot that is not live
+          const int top = __reduce_max_sync(0xffffffffu, __float2int_ru(s[h]) + ev);      // (-inf: the least integer)
           if (top > J[h] + 2) {
             f[h] = exp2_fast((float)(J[h] - top));
             J[h] = top;
@@ -809,8 +812,8 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
 #pragma unroll
       for (int h = 0; h < GT; ++h)
         if (GT == 1 || h < G) {
-          // (no live slot so far: m_own is -inf; a NaN stays one, and the sums with it)
-          const float p = s[h] == -INFINITY ? 0.f : exp2_fast(s[h] - m_own[h]), y = p * pow2((int)m_own[h] - (J[h] - 126 - X_TOP));
+          // (a NaN stays one, and the sums with it)
+          const float p = exp2_fast(s[h]), y = p * pow2(126 + X_TOP - J[h]);
           l_run[h] += p;
 #pragma unroll
           for (int i = 0; i < PG; ++i) {
@@ -905,9 +908,9 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
         if (h == hc) { mo = m_own[h]; j = J[h]; }
 #pragma unroll
       for (int k = 1; k <= WARPS; ++k) m = fmaxf(m, part_m[k][hc]);
-      const bool any = hc < G && mo > -INFINITY;
+      const bool any = hc < G && part_m[wid][hc] > -INFINITY;
       fm[x] = any ? exp2_fast(mo - m) : 0.f;
-      fo[x] = any ? fm[x] * pow2(j - 126 - X_TOP + (INT ? 0 : CODE_EXP) - (int)mo) : 0.f;
+      fo[x] = any ? fm[x] * pow2(j - 126 - X_TOP + (INT ? 0 : CODE_EXP)) : 0.f;
     }
     {
       constexpr int LOW = N == 2 ? 1 : 2;    // (neighbouring lanes have halves of a slot's groups with N == 1)

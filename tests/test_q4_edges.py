@@ -76,6 +76,33 @@ def test_logits_beside_a_channel_of_large_queries(dtype, G):
     assert (got - pm).norm() <= 9.7e-6 * pm.norm(), float((got - pm).norm() / pm.norm())
 
 
+# ------------------------------------------------------------------------------------------------ magnitudes
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("G", [1, 4, 8])
+@pytest.mark.parametrize("size", [1e3, 1e6, -1e6, 1e12, -1e12])
+def test_logits_of_any_size(dtype, G, size):
+    """Equal logits of size * 1e6 / sqrt(d), the incoming token's below them: the mean of the rows."""
+    V, units, B, d = P.vatp(), 3, 700, 64
+    p, g = _params(dtype, 1, units * G, units if G > 1 else 0, d, B=B), _gen(14)
+    k, v = torch.zeros(units, B, d, device="cuda"), torch.randn(units, B, d, generator=g, device="cuda")
+    k[..., 0] = 1e6
+    c = _packed(p, k, v)
+    c.acc.zero_()
+    ref = _reference(c, p)
+    q = torch.zeros(1, units * G, d, device="cuda", dtype=DT[dtype])
+    q[..., 0] = size
+    k1, v1 = torch.zeros(1, units, d, device="cuda", dtype=q.dtype), torch.randn(1, units, d, generator=g, device="cuda").to(q.dtype)
+    k1[..., 0] = 0.0 if size > 0 else 2e6
+    out = torch.empty_like(q)
+    V.vatp_decode_step_q4(p, c, q, k1, v1, out)
+    torch.cuda.synchronize()
+    want, v_mag = ref.v[:, :B].mean(1, keepdim=True), ref.mag[1][:, :B].mean(1).repeat_interleave(32, -1)[:, None]
+    off = (out.double().view(units, G, d) - want).abs()
+    # sums of 700 terms in 32 bits, p sc in two halves, the exponential's 2^-22; half a step of the output
+    assert torch.all(off <= 2.0 ** -19 * v_mag + torch.finfo(q.dtype).eps / 2 * want.abs())
+    assert torch.all((c.acc.view(units, -1)[:, :B] * B - 1).abs() <= 2.0 ** -19) and torch.all(c.acc[:, :, B] == 0)
+
+
 # ------------------------------------------------------------------------------------------------ values that are not finite
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
 @pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f32", 64)])
