@@ -761,10 +761,11 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
 #pragma unroll
         for (int i = 0; i < PG; ++i) pr[i] = 0u;
       }
-      float most = 0.f;                      // 126 + exponent of the largest scale, rounded up (a scale of 0 counts as 2^-96)
+      // 126 + exponent of the largest scale, rounded up (scales below 2^-94 count as that: with J 2 less, 2^(J - 29) is then still a normal number)
+      float most = 0.f;
 #pragma unroll
       for (int i = 0; i < PG; ++i) most = fmaxf(most, q4_scale(pr[i]));
-      const int ev = max((int)(__float_as_uint(most) >> 23), 30);
+      const int ev = max((int)(__float_as_uint(most) >> 23), 32);
 #pragma unroll
       for (int h = 0; h < GT; ++h) {
         f[h] = 1.f;

@@ -103,6 +103,28 @@ def test_logits_of_any_size(dtype, G, size):
     assert torch.all((c.acc.view(units, -1)[:, :B] * B - 1).abs() <= 2.0 ** -19) and torch.all(c.acc[:, :, B] == 0)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("G", [1, 4])
+def test_values_as_small_as_the_format_holds(dtype, G):
+    """Scales of 2^-99, the largest probabilities in a warp's later items."""
+    V, units, B, d = P.vatp(), 160, 600, 64
+    p, g = _params(dtype, 1, units * G, units if G > 1 else 0, d, B=B), _gen(15)
+    k = torch.zeros(units, B, d, device="cuda")
+    k[:, :, 0] = torch.linspace(0.0, 1.0, B, device="cuda")
+    v = torch.randint(0, 16, (units, B, d), generator=g, device="cuda") * 2.0 ** -99
+    v[..., ::32], v[..., 1::32] = 0.0, 15 * 2.0 ** -99                             # lo 0, sc 2^-99
+    c = _packed(p, k, v)
+    q = torch.zeros(1, units * G, d, device="cuda", dtype=DT[dtype])
+    q[..., 0] = 24.0                                                               # (logits 0 to 4.3, in powers of two)
+    k1, v1, out = torch.zeros(1, units, d, device="cuda", dtype=q.dtype), v[:, 3][None].to(q.dtype).contiguous(), torch.empty_like(q)
+    want, _, _, _, rel, v_mag = _reference(c, p).step(q.view(units, G, d), k1.view(units, d), v1.view(units, d))
+    V.vatp_decode_step_q4(p, c, q, k1, v1, out)
+    torch.cuda.synchronize()
+    off = (out.double().view(want.shape) - want).abs()
+    # (p sc of a warp's largest is held to 2^-24 at least where it is this small)
+    assert torch.all(off <= (rel[..., None] + 2.0 ** -20) * v_mag + torch.finfo(q.dtype).eps / 2 * want.abs())
+
+
 # ------------------------------------------------------------------------------------------------ values that are not finite
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
 @pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f32", 64)])
