@@ -39,8 +39,7 @@
 #include <cooperative_groups.h>
 #include <cuda_fp16.h>
 
-#include <atomic>
-
+#include "known_counts.h"
 #include "q4.cuh"
 
 namespace cg = cooperative_groups;
@@ -1098,34 +1097,33 @@ decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int 
   }
 }
 
-// How many clusters of `split` CTAs with an SM each run at once (they lie within a GPC, which is not a multiple of them); looked up
-// once per device and size.
+// How many clusters of `split` CTAs with an SM each run at once (they lie within a GPC, which is not a multiple of them); asked for
+// once per device and size.  0 where the runtime does not say: a unit then stays on fewer CTAs in this call.
+using ClusterCounts = KnownCounts<16, Q4_SPLIT + 1>;
 template <typename Kernel>
-int clusters_at_once(Kernel kern, int split, int threads, size_t dyn) {
-  static std::atomic<int> known[16][Q4_SPLIT + 1];
+int clusters_at_once(ClusterCounts& known, Kernel kern, int split, int threads, size_t dyn) {
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return 0;
-  std::atomic<int>* entry = dev < 16 ? &known[dev][split] : nullptr;
-  if (entry && entry->load()) return entry->load() - 1;
-  if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)dyn) != cudaSuccess ||
-      cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) {
-    cudaGetLastError();
-    return 0;
-  }
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)split);
-  cfg.blockDim = dim3((unsigned)threads);
-  cfg.dynamicSmemBytes = dyn;
-  cudaLaunchAttribute attr;
-  attr.id = cudaLaunchAttributeClusterDimension;
-  attr.val.clusterDim.x = split;
-  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
-  int n = 0;
-  if (cudaOccupancyMaxActiveClusters(&n, kern, &cfg) != cudaSuccess) { cudaGetLastError(); n = 0; }
-  if (entry) entry->store(n + 1);
-  return n;
+  return known.get(dev, split, [&] {
+    int n = 0;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)split);
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = dyn;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = split;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)dyn) != cudaSuccess ||
+        cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess ||
+        cudaOccupancyMaxActiveClusters(&n, kern, &cfg) != cudaSuccess) {
+      cudaGetLastError();
+      return -1;
+    }
+    return n;
+  });
 }
 
 template <typename T, int HD, int GT>
@@ -1140,18 +1138,19 @@ cudaError_t launch_gt(int units, int G, int B, int F, int R, int window, int nor
   auto kern8 = win ? decode_q4_kernel<T, HD, true, GT, 8, true> : decode_q4_kernel<T, HD, false, GT, 8, true>;
   auto pair8 = win ? decode_q4_kernel<T, HD, true, GT, 8, false> : decode_q4_kernel<T, HD, false, GT, 8, false>;
   const size_t most16 = 226 * 1024 - fixed16, most8 = 226 * 1024 - fixed8;
+  static ClusterCounts known[2];         // (of kern16, without and with a history)
   // Units on fewer CTAs than SMs: an SM to a CTA (two of a launch on one SM while others idle: 32 units x 2049 slots, four CTAs each,
   // 8.0 and 7.3 us per step, with the same kernel), a power of two of them per unit that run at once and find some slots, of sixteen warps when there
   // are more than three rounds for eight (74 units x 4097: 15.7 and 14.0 us; 32 x 1025: 6.0 and 6.8, which is why not always).  More units
   // than SMs: one CTA of eight warps each, two on an SM.
   int split = 1;
-  while (split < Q4_SPLIT && units * split * 2 <= sms && cap / split >= 4 * Q4_ROWS && clusters_at_once(kern16, split * 2, 17 * 32, most16) >= units) split *= 2;
+  while (split < Q4_SPLIT && units * split * 2 <= sms && cap / split >= 4 * Q4_ROWS && clusters_at_once(known[win], kern16, split * 2, 17 * 32, most16) >= units) split *= 2;
   // Then any other number that saves the warps a round: clusters lie within a GPC, seven of sixteen CTAs run at once, fifteen of eight, but
   // eleven of ten, 22 of six (16 units x 4002 slots, four heads: four CTAs each 12.8 us per step, six 10.7; 40 x 2049: two 9.1, three 7.7).
   // Of clusters of three and of five, the last two of those said to fit have been seen to wait (of three, 43 units 7.7 us and 45 10.4).
   auto rounds_of = [&](int split) { return (B + 1 - Q4_EXTRA + 8 * Q4_ROWS * split - 1) / (8 * Q4_ROWS * split); };
   for (int more = split + 1; more <= Q4_SPLIT && units * more <= sms; ++more)
-    if (rounds_of(more) < rounds_of(split) && clusters_at_once(kern16, more, 17 * 32, most16) >= units + (more & 1) * 2) split = more;
+    if (rounds_of(more) < rounds_of(split) && clusters_at_once(known[win], kern16, more, 17 * 32, most16) >= units + (more & 1) * 2) split = more;
   const bool alone = units <= sms;
   // a ring takes the warp's partial output in the end
   const int least = (G * HD * 4 + ITEM - 1) / ITEM > 2 ? (G * HD * 4 + ITEM - 1) / ITEM : 2;
