@@ -186,10 +186,10 @@ compact_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
 
 // Windowed indicator state: ring[u][(T - w + r) mod w][slot] = win_rows[u][r][kept[slot]] and the
 // exact fixed-point window sum of every slot (Eq. 3).
-__global__ void ring_kernel(int units, int T, int w, int B, int cap, const float* __restrict__ win_rows,
+__global__ void ring_kernel(int T, int w, int B, int cap, const float* __restrict__ win_rows,
                             const int32_t* __restrict__ kept, vatp_cache c, int32_t* dev_status) {
-  const int u = blockIdx.y;
-  const int slot = blockIdx.x * blockDim.x + threadIdx.x;
+  const int per_unit = (cap + blockDim.x - 1) / blockDim.x, u = blockIdx.x / per_unit;
+  const int slot = (blockIdx.x - u * per_unit) * blockDim.x + threadIdx.x;
   if (slot >= cap) return;
   const int len = min(T, B);
   int src = slot < len ? kept[(int64_t)u * B + slot] : -1;
@@ -208,6 +208,14 @@ __global__ void ring_kernel(int units, int T, int w, int B, int cap, const float
 }
 
 }  // namespace
+
+cudaError_t launch_ring(const Shape& s, int B, const float* win_rows, const int32_t* kept, const vatp_cache& c, int32_t* dev_status, cudaStream_t st) {
+  const int cap = cache_capacity(B);
+  const int64_t ctas = (int64_t)s.units * ((cap + 127) / 128);
+  if (ctas > 0x7fffffffll) return cudaErrorInvalidValue;
+  ring_kernel<<<(unsigned)ctas, 128, 0, st>>>(s.T, s.window, B, cap, win_rows, kept, c, dev_status);
+  return cudaGetLastError();
+}
 
 cudaError_t launch_compact(const Shape& s, int dtype, int B, const void* k, const void* v, const float* attn_acc,
                            const float* vnorm, const float* win_rows, const int32_t* kept, const vatp_cache& c,
@@ -243,10 +251,7 @@ cudaError_t launch_compact(const Shape& s, int dtype, int B, const void* k, cons
   e = cudaLaunchKernelEx(&dl.cfg, compact_kernel, tm_k, tm_v, rs, s, eb, B, cap, (const char*)k, (const char*)v, attn_acc,
                          vnorm, kept, c, rows_pb, nbuf, s.window > 0 && !win_rows ? 1 : 0, dev_status);
   if (e != cudaSuccess) return e;
-  if (s.window > 0 && win_rows) {
-    ring_kernel<<<dim3((cap + 127) / 128, s.units), 128, 0, st>>>(s.units, s.T, s.window, B, cap, win_rows, kept, c, dev_status);
-    e = cudaGetLastError();
-  }
+  if (s.window > 0 && win_rows) e = launch_ring(s, B, win_rows, kept, c, dev_status, st);
   return e;
 }
 

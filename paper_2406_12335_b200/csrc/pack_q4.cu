@@ -188,26 +188,6 @@ unpack_q4_kernel(const __grid_constant__ CopyPlan plan, int row_ctas, int64_t sl
     }
 }
 
-// Windowed indicator state of the kept tokens, as compact.cu's ring_kernel leaves it: ring[u][(T - w + r) mod w][slot] =
-// win_rows[u][r][kept[slot]] and the exact fixed-point sum of every slot.
-__global__ void ring_q4_kernel(int T, int w, int B, int cap, const float* __restrict__ win_rows, const int32_t* __restrict__ kept,
-                               vatp_cache c, int32_t* dev_status) {
-  const int per_unit = (cap + blockDim.x - 1) / blockDim.x, u = blockIdx.x / per_unit;
-  const int slot = (blockIdx.x - u * per_unit) * blockDim.x + threadIdx.x;
-  if (slot >= cap) return;
-  int src = slot < min(T, B) ? kept[(int64_t)u * B + slot] : -1;
-  if (src >= 0 && !VATP_INB(src, T, dev_status)) src = -1;
-  long long fx = 0;
-  for (int r = 0; r < w; ++r) {
-    const int j = T - w + r;                 // query position of this window row (may be < 0)
-    const float p = src >= 0 && j >= 0 ? win_rows[((int64_t)u * w + r) * T + src] : 0.f;
-    c.ring[((int64_t)u * w + ((j % w) + w) % w) * cap + slot] = p;
-    fx += prob_to_fixed(p);
-  }
-  c.acc_fixed[(int64_t)u * cap + slot] = fx;
-  c.acc[(int64_t)u * cap + slot] = fixed_to_prob(fx);
-}
-
 template <typename T, int HD>
 cudaError_t pack_hd(const Shape& s, int B, const void* k, const void* v, const int32_t* kept, const CacheArray* arrays, int n, const vatp_cache& a,
                     const float* attn_acc, const float* vnorm, const vatp_cache_q4& c, int32_t* dev_status, cudaStream_t st) {
@@ -241,13 +221,7 @@ cudaError_t launch_compact_q4(const Shape& s, int dtype, int B, const void* k, c
   auto f = dtype == VATP_F32 ? (s.d == 64 ? pack_hd<float, 64> : pack_hd<float, 128>)
                              : (s.d == 64 ? pack_hd<__nv_bfloat16, 64> : pack_hd<__nv_bfloat16, 128>);
   cudaError_t e = f(s, B, k, v, kept, nullptr, 0, c.state, attn_acc, vnorm, c, dev_status, st);
-  if (e == cudaSuccess && s.window > 0) {
-    const int cap = cache_capacity(B);
-    const int64_t ctas = (int64_t)s.units * ((cap + 127) / 128);
-    if (ctas > 0x7fffffffll) return cudaErrorInvalidValue;
-    ring_q4_kernel<<<(unsigned)ctas, 128, 0, st>>>(s.T, s.window, B, cap, win_rows, kept, c.state, dev_status);
-    e = cudaGetLastError();
-  }
+  if (e == cudaSuccess && s.window > 0) e = launch_ring(s, B, win_rows, kept, c.state, dev_status, st);
   return e;
 }
 

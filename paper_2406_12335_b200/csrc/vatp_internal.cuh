@@ -155,6 +155,8 @@ cudaError_t launch_select(int units, int T, int B, int F, int R, const float* sc
 cudaError_t launch_compact(const Shape& s, int dtype, int B, const void* k, const void* v, const float* attn_acc,
                            const float* vnorm, const float* win_rows, const int32_t* kept, const vatp_cache& c,
                            int32_t* dev_status, cudaStream_t st);
+// windowed decode state (of either form) from the prompt's probability rows: ring, acc_fixed, acc
+cudaError_t launch_ring(const Shape& s, int B, const float* win_rows, const int32_t* kept, const vatp_cache& c, int32_t* dev_status, cudaStream_t st);
 // windowed decode state from Q, the compacted keys and the row normalisers (natural log): ring, acc_fixed, acc
 // (G: query heads per KV head; s describes the KV units, q and lse hold G times as many heads)
 cudaError_t launch_window_ring(const Shape& s, int G, int dtype, int B, const void* q, const float* lse, const vatp_cache& c,
