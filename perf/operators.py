@@ -296,6 +296,8 @@ def prepare(case, seed):
         st["kept"] = _kept(case, seed, b, B)
         st["vnorm"] = st["v"].float().abs().sum(-1)
         st["win_rows"] = _history(case, seed, b, T) if case["window"] else None
+        if case["window"] > T:                           # (queries before the prompt's first: rows of zeros)
+            st["win_rows"][:, :, :case["window"] - T] = 0
         st["attn_acc"] = st["win_rows"].sum(2) if case["window"] else _indicator(case, seed, b, T)
         st["to"] = _empty_state(case, q4=True)
         st["rows"] = _empty_state(case, q4=False, like=st["to"])
