@@ -5,7 +5,7 @@ import torch
 
 from tests import parity as P
 from tests import q4_reference as Q
-from tests.test_q4 import DT, _filled, _gen, _params, _rows, _status
+from tests.test_q4 import DT, _arrays, _clone, _filled, _gen, _params, _rows, _status
 
 pytestmark = pytest.mark.gpu
 
@@ -197,3 +197,82 @@ def test_a_nan_reaches_the_outputs(dtype, G, d, B, where):
     slot = c.free_slot.view(-1).long()
     u = torch.arange(units, device="cuda")
     assert torch.all(may_go[u, slot]) and not torch.any(live[u, slot])
+
+
+# ------------------------------------------------------------------------------------------------ copies
+@pytest.mark.parametrize("form", ["q4", "wide"])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_copies_of_more_entries_than_a_warp_has_lanes(form, in_place):
+    """Entries that take the same source lie more than 32 apart, the first of them beyond the first 32 or not."""
+    V, n = P.vatp(), 101
+    p = _params("bf16", n, 2, 0, 64, B=23)
+    src = _filled(p, 23, seed=1, form=form)
+    src.next_pos.copy_(torch.arange(2 * n, device="cuda").view(n, 2) + 1000)
+    dst = src if in_place else _filled(p, 23, seed=2, form=form)
+    before_src, before = _clone(src, p), _clone(dst, p)
+    m = [V.SEQ_KEEP] * n
+    for b in (1, 2, 31, 32, 33, 64, 100):
+        m[b] = 40                                                                  # entries before and behind their source
+    for b in (35, 70, 99):
+        m[b] = 5                                                                   # the first taker in the second 32
+    m[98], m[97], m[96] = 66, V.SEQ_FREE, 96
+    status = _status()
+    V.vatp_cache_copy(p, src, dst, torch.tensor(m, dtype=torch.int32, device="cuda"), dev_status=status)
+    torch.cuda.synchronize()
+    assert int(status) == 0
+    for name, t in _arrays(dst).items():
+        for b, j in enumerate(m):
+            if j == V.SEQ_FREE:
+                if name in ("pos", "last_slot"):
+                    assert torch.all(t[b] == -1)
+                elif name in ("len", "free_slot", "next_pos"):
+                    assert torch.all(t[b] == 0)
+            else:
+                want = getattr(before, name)[b] if j == V.SEQ_KEEP else getattr(before_src, name)[j]
+                assert torch.equal(t[b], want), (name, b)
+
+
+def _whole(g, *shape, dtype):
+    """Rows that both forms hold exactly: whole numbers, -8 and 7 in every group (lo -8, sc 1)."""
+    x = torch.randint(-8, 8, shape, generator=g, device="cuda").to(DT[dtype])
+    x[..., ::32], x[..., 5::32] = -8, 7
+    return x
+
+
+@pytest.mark.parametrize("dtype,h,kv,d,window", [("bf16", 4, 0, 128, 0), ("bf16", 8, 2, 64, 0), ("f32", 3, 0, 64, 0), ("bf16", 4, 0, 64, 6), ("f32", 4, 2, 128, 6)])
+def test_freed_and_joined_entries_go_on_generating_in_either_form(dtype, h, kv, d, window):
+    """One entry freed, one joined from a smaller budget, one kept: 16- or 32-bit steps and 4-bit steps on the same values."""
+    V, hk, g = P.vatp(), kv or h, _gen(16)
+    pf, pt = (_params(dtype, n, h, kv, d, B=B, F=1, R=2, window=window) for n, B in ((1, 20), (3, 23)))
+    states = []
+    for p, n in ((pf, 20), (pt, 23)):
+        wide, c = _filled(p, n, form="wide"), V.CacheQ4(p)
+        for x in (wide.k_cache, wide.v_cache):
+            x[:, :, :n] = _whole(g, *x[:, :, :n].shape, dtype=dtype)
+        V.vatp_cache_pack_q4(p, wide, c)
+        states.append((wide, c))
+    m = torch.tensor([V.SEQ_FREE, 0, V.SEQ_KEEP], dtype=torch.int32, device="cuda")
+    (src, src4), (dst, dst4) = states
+    V.vatp_cache_copy(pt, src, dst, m)
+    V.vatp_cache_copy(pt, src4, dst4, m)
+    status, eps = _status(), torch.finfo(DT[dtype]).eps / 2
+    for i in range(12):
+        q = torch.randn(3, h, d, generator=g, device="cuda").to(DT[dtype])
+        k, v = (_whole(g, 3, hk, d, dtype=dtype) for _ in range(2))
+        got = []
+        for step, c in ((V.vatp_decode_step, dst), (V.vatp_decode_step_q4, dst4)):
+            out, evicted = torch.empty_like(q), torch.empty(3, hk, dtype=torch.int32, device="cuda")
+            step(pt, c, q, k, v, out, evicted_pos=evicted, dev_status=status)
+            got.append((out.double(), evicted))
+        torch.cuda.synchronize()
+        (o, e), (o4, e4) = got
+        assert int(status) == 0
+        if i == 0:                                                                 # the freed entry's only token
+            assert torch.equal(o[0].view(hk, -1, d), v[0].double()[:, None].expand(hk, h // hk, d))
+        # each side: its own rounding; p in 16 bits or more (2^-16 of values up to 8); logits, sums of d products up to 8 * 4.5, to
+        # 2^-23 d 36 / sqrt(d) of a probability
+        assert torch.all((o - o4).abs() <= eps * (o.abs() + o4.abs()) + 2 * 8 * (2.0 ** -16 + 2.0 ** -23 * 36 * d ** 0.5))
+        assert torch.equal(e, e4)
+        for name in ("pos", "len", "free_slot", "next_pos", "last_slot"):
+            assert torch.equal(getattr(dst, name), getattr(dst4, name)), name
+    assert dst.next_pos[0].tolist() == [12] * hk and dst.len.flatten().tolist() == [12] * hk + [23] * hk * 2
