@@ -347,8 +347,9 @@ vatp_status vatp_cache_unpack_q4(const vatp_params* params, const vatp_cache_q4*
  * row; its norm (Eq. 4) is that of k_new's and v_new's values as given.  A NaN in q_new or in a row that holds a token makes those
  * outputs and indicators NaN that depend on it (with a history window the sums then mean nothing until it has left).  Up to eight query heads per KV head
  * (VATP_ERR_UNSUPPORTED beyond, and for budgets whose logits do not fit into the shared memory of the CTAs of a unit).
- * Everything else is as in vatp_decode_step, except that VATP_FLAG_DECODE_OVERLAP has no effect: every step waits for all earlier
- * work in the stream.
+ * Everything else is as in vatp_decode_step without VATP_FLAG_DECODE_OVERLAP, which has no effect here: the step requests K rows ahead
+ * of the end of earlier work in the stream, under the assumption stated there about who writes cache rows, and reads everything else, and
+ * writes, after it.
  */
 vatp_status vatp_decode_step_q4(const vatp_params* params, const vatp_cache_q4* cache, const void* q_new,
                                 const void* k_new, const void* v_new, void* out, int32_t* evicted_pos,

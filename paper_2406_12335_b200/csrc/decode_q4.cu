@@ -32,9 +32,9 @@
 //   * The CTA joins its partials, the cluster those of its CTAs by st.async into the partners' shared memory; every CTA then updates the
 //     indicators of its own slots, and every warp sends its eviction candidate to rank 0.
 // What bounds it (one head, d 128): instructions and their latency, not memory.  An item's two products are 645 instructions of a warp
-// (110 of them requests) for 5 KB, and a step has some 1000 more per warp that do not depend on its length.  32 units x 2049 slots: 6.2 us
+// (110 of them requests) for 5 KB, and a step has some 1000 more per warp that do not depend on its length.  32 units x 2049 slots: 6.3 us
 // per step in a chain of steps, of which the time between launches takes 0.7, q 0.85, two items' K 0.8, V 1.25, joining partials, CTAs and candidates
-// 2.6; 256 units x 1639: 16.9 us, 4.4 TB/s.  Not faster: a warp that requests all rings' items; three CTAs an SM (72 registers spill); p sc of the next
+// 2.6; 256 units x 1639: 16.7 us, 4.4 TB/s.  Not faster: a warp that requests all rings' items; three CTAs an SM (72 registers spill); p sc of the next
 // item formed while this one's products run (spills with eight warps in pairs: 18.7 -> 21.5 us; without spills 6.74 -> 6.97).
 #include <cooperative_groups.h>
 #include <cuda_fp16.h>
@@ -240,7 +240,7 @@ __device__ __forceinline__ unsigned long long min_key(unsigned long long key) {
 // slices received [2 G HD at most] | logits [G][ld].
 template <int HD> constexpr int q4_item = Q4_ROWS * (HD / 2 + HD / 8);      // bytes of an item: codes, then parameters
 
-// ALONE: one CTA on an SM (eight warps then have 140 registers instead of 96: 32 units x 2049 slots 7.3 -> 6.8 us).
+// ALONE: one CTA on an SM (eight warps then have 128 registers and more instead of 96: 32 units x 2049 slots 7.3 -> 6.8 us).
 template <typename T, int HD, bool WINDOWED, int GT, int WARPS, bool ALONE>
 __global__ void __launch_bounds__(WARPS * 32 + 32, ALONE ? 1 : 2)
 decode_q4_kernel(int G_arg, int split, int chunk, int ld, int depth, int B, int cap, int F, int R, int w, int norm, float scale_log2, vatp_cache_q4 c, const T* q_new,
@@ -1145,7 +1145,7 @@ cudaError_t launch_gt(int units, int G, int B, int F, int R, int window, int nor
   // than SMs: one CTA of eight warps each, two on an SM.
   int split = 1;
   while (split < Q4_SPLIT && units * split * 2 <= sms && cap / split >= 4 * Q4_ROWS && clusters_at_once(known[win], kern16, split * 2, 17 * 32, most16) >= units) split *= 2;
-  // Then any other number that saves the warps a round: clusters lie within a GPC, seven of sixteen CTAs run at once, fifteen of eight, but
+  // Then any other number that would save eight warps a round (CTAs that get sixteen below have fewer): clusters lie within a GPC, seven of sixteen CTAs run at once, fifteen of eight, but
   // eleven of ten, 22 of six (16 units x 4002 slots, four heads: four CTAs each 12.8 us per step, six 10.7; 40 x 2049: two 9.1, three 7.7).
   // Of clusters of three and of five, the last two of those said to fit have been seen to wait (of three, 43 units 7.7 us and 45 10.4).
   auto rounds_of = [&](int split) { return (B + 1 - Q4_EXTRA + 8 * Q4_ROWS * split - 1) / (8 * Q4_ROWS * split); };
